@@ -248,6 +248,99 @@ int ls_decode_attend(ls_ctx* ctx, const ls_shape* shape, int32_t cap, int32_t T,
 size_t ls_decode_workspace_bytes(const ls_shape* shape, int32_t cap, int32_t T);
 
 /*
+ * ---- Paged caches and packed sequences ---------------------------------------------------------------------------
+ * The calls below serve dialogues whose keys and values live in pages and whose lengths differ within a batch: attention
+ * of whole prompts packed one behind the other, rows into and out of the pages, and a token over them.
+ */
+
+/* Rows of `H` heads of `d` neighbouring values each, as a caller's tensor holds them.  Sequence s's row i of head h begins
+ * at element s * seq + i * row + h * head of `data`; packed sequences follow each other (s * seq is left out, i counts on
+ * from starts[s]).  Strides are in elements, not negative, and multiples of 16 bytes; `data` is 16-byte aligned.  Rows that a call
+ * writes may not overlap. */
+typedef struct {
+    void* data;
+    int64_t seq, row, head;
+} ls_rows;
+
+typedef enum { LS_CACHE_BF16 = 0, LS_CACHE_E4M3 = 1 } ls_cache_type;
+
+/* A pool of pages.  Page p holds `page` neighbouring positions of one sequence, of all KV heads: k, v [pages,Hkv,page,d],
+ * contiguous, 16-byte aligned.  LS_CACHE_BF16: bf16.  LS_CACHE_E4M3: 8-bit floats (1 sign, 4 exponent, 3 fraction bits, bias 7, no
+ * infinities, 0x7F and 0xFF are NaN) and, in k_exp, v_exp [pages,Hkv,page], a byte E for each row: a stored value stands
+ * for code * 2^(E - 127), which bf16 and fp32 hold exactly.
+ * Where a sequence's pages are is a row of `table` [B,max_pages] int32, device memory: positions p * page .. of sequence b lie in
+ * page table[b][p].  Several sequences may share pages that are read.  A page number outside [0, pages), and a position beyond max_pages * page, is nowhere:
+ * rows of it are neither written nor read, keys of it are not seen, and LS_STAT_PAGE_RANGE is set. */
+typedef struct {
+    int32_t Hkv, d;          /* d in {64, 128} */
+    int32_t page;            /* positions of a page: 16, 32, 64, 128 or 256 */
+    int32_t type;            /* ls_cache_type */
+    int64_t pages;           /* 1 <= pages < 2^31 */
+    void *k, *v;
+    uint8_t *k_exp, *v_exp;  /* LS_CACHE_E4M3 only */
+} ls_cache;
+
+/*
+ * ls_packed_prefill -- causal attention of whole prompts, or of the new rows of later turns, without a selection of lines
+ * (Sec. 2.2 with M[a][b] = 1 iff b <= p_a), for sequences of different lengths:
+ *     out[a] = sum_b softmax_b(scale * <q_a, k_b>) v_b.
+ *
+ *   shape: B sequences, Hq, Hkv, d, dtype, scale.  n: rows of k and v, n_hat: rows of q and out.  w is ignored.
+ *   q_starts, k_starts [B+1] int32, device memory: rows q_starts[s] .. q_starts[s+1] - 1 are sequence s's queries, likewise its
+ *        keys; n and n_hat count all sequences' rows then.  Both NULL: every sequence has n keys and n_hat queries.
+ *   The queries are the last positions of their sequence: query i of m sees the keys up to (keys of the sequence) - m + i,
+ *        none where that is negative.  A sequence whose starts descend or leave [0, n] or [0, n_hat] is passed by, with
+ *        all behind it (LS_STAT_STARTS).
+ * Outputs:
+ *   out in dtype; a row that sees no key is all zeros.  Rows of no sequence stay as they are.
+ *   lse fp32 or NULL, [Hq,n_hat] (packed) or [B,Hq,n_hat]: natural log of the softmax denominator (-inf without a key)
+ * Workspace: ls_packed_workspace_bytes (0 for an invalid shape); less is enough where the rows fill the chip, and slower elsewhere.
+ */
+int ls_packed_prefill(ls_ctx* ctx, const ls_shape* shape, const ls_rows* q, const ls_rows* k, const ls_rows* v,
+                      const int32_t* q_starts, const int32_t* k_starts, const ls_rows* out, float* lse, void* hip_stream);
+size_t ls_packed_workspace_bytes(const ls_shape* shape);
+
+/*
+ * ls_cache_write -- rows of K and V into the pages of their sequences; ls_cache_read -- the way back, in order, for the calls
+ * that take whole contexts (ls_score, ls_sparse_prefill, ls_kv_compress).
+ *
+ *   shape: B sequences, Hkv and d of the cache, dtype of the rows (LS_BF16 or LS_F32).  n_hat: rows of k and of v.  Hq, n, w, scale
+ *        are ignored.
+ *   starts [B+1] int32, device memory: rows starts[s] .. starts[s+1] - 1 are sequence s's (n_hat counts all rows); a sequence whose
+ *        starts descend or leave [0, n_hat] is passed by, with all behind it (LS_STAT_STARTS).  NULL: each sequence has n_hat rows of its own.
+ *   count [B] int32, device memory: only the first count[s] of them (clamped to [0, n_hat]); NULL: all.  Not with starts.
+ *   pos [B] int32, device memory: the position in the cache at which sequence s's rows begin; NULL: 0.
+ * ls_cache_write: bf16 pages hold the rows rounded to nearest even.  E4M3: E is the smallest byte from 10 to 247 with
+ *   max |x| <= 448 * 2^(E-127) over the row's finite values, the codes are x * 2^(127-E) rounded to nearest even; infinities and
+ *   NaN become NaN.  What else is in the pages stays.  Rows that meet in one place (a page that is twice in the table) leave one of the values of each there.
+ * ls_cache_read: rows past count and rows that are nowhere stay as they are.
+ * No workspace.
+ */
+int ls_cache_write(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, const ls_rows* k, const ls_rows* v,
+                   const int32_t* starts, const int32_t* count, const int32_t* table, int32_t max_pages,
+                   const int32_t* pos, void* hip_stream);
+int ls_cache_read(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, const ls_rows* k, const ls_rows* v,
+                  const int32_t* starts, const int32_t* count, const int32_t* table, int32_t max_pages,
+                  const int32_t* pos, void* hip_stream);
+
+/*
+ * ls_paged_attend -- ls_decode_attend over pages: the newest token's query of each sequence attends over the first len[b]
+ * positions of its cache.
+ *
+ *   shape: B, Hq, Hkv, d, scale, dtype (LS_BF16 only); n: no sequence is longer (lengths are clamped to [0, min(n, max_pages *
+ *        page)], with LS_STAT_PAGE_RANGE where that is less than len).  n_hat, w are ignored.  Hq/Hkv <= 32.
+ *   q [B,Hq,d];  table [B,max_pages], len [B] int32, device memory
+ * Outputs:
+ *   out [B,Hq,d] in dtype; all zeros where there is no key
+ *   lse [B,Hq] fp32 or NULL: natural log of the softmax denominator (-inf when there is no key)
+ * Workspace: ls_paged_workspace_bytes (0 for an invalid shape).  What this header says of calls of ls_decode_attend that overlap holds for
+ * these too: they share its counters.
+ */
+int ls_paged_attend(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, const void* q,
+                    const int32_t* table, int32_t max_pages, const int32_t* len, void* out, float* lse, void* hip_stream);
+size_t ls_paged_workspace_bytes(const ls_shape* shape);
+
+/*
  * Timing of the sparse attention itself (the dominant part of ls_sparse_prefill), for roofline
  * reports.  After ls_profile_enable(ctx, 1) every ls_sparse_prefill call attaches a pair of HIP
  * events to the launch of the attention kernel and, where long row blocks may have been cut into
@@ -276,6 +369,10 @@ int ls_profile_prefill_kernel_ms(ls_ctx* ctx, double* mean_ms, int32_t* launches
 #define LS_STAT_V_INVALID   16  /* ls_sparse_prefill: a head's v_idx was not strictly ascending inside [0, n); that
                                    head's columns were ignored (its diagonals still apply) */
 #define LS_STAT_MERGE_RANGE 32  /* ls_merge_lines: input entries outside [0, n) were dropped */
+#define LS_STAT_PAGE_RANGE  64  /* ls_cache_write, ls_cache_read, ls_paged_attend: a position lies in no page of the pool or beyond
+                                   the table; it was left out */
+#define LS_STAT_STARTS     128  /* ls_packed_prefill, ls_cache_write, ls_cache_read: a sequence's starts descend or leave the rows;
+                                   it was passed by, with all behind it */
 int ls_poll_status(ls_ctx* ctx, int32_t* host_out, void* hip_stream);
 
 #ifdef __cplusplus

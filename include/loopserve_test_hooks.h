@@ -69,6 +69,35 @@ int ls_debug_prefill_in_pieces(const ls_shape* shape);
  */
 int ls_debug_score_route(const ls_shape* shape, int32_t mode, int32_t positions, int32_t route[9], int64_t* begins);
 
+/*
+ * What the calls on pages and packed sequences check before they launch, without a context or a GPU: the status that the call of the same arguments would
+ * return for them (pointers are looked at, not followed; write: 1 ls_cache_write, 0 ls_cache_read).
+ */
+int ls_debug_check_packed(const ls_shape* shape, const ls_rows* q, const ls_rows* k, const ls_rows* v, const int32_t* q_starts, const int32_t* k_starts,
+                          const ls_rows* out, const float* lse);
+int ls_debug_check_move(const ls_shape* shape, const ls_cache* cache, const ls_rows* k, const ls_rows* v, const int32_t* starts, const int32_t* count,
+                        const int32_t* table, int32_t max_pages, const int32_t* pos, int32_t write);
+int ls_debug_check_paged(const ls_shape* shape, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages, const int32_t* len,
+                         const void* out, const float* lse);
+
+/* The page (of `pages` of `page` positions) that the kernels take position `pos` of sequence b to lie in, -1 for none; `table` is host memory here. */
+int ls_debug_page_of(const int32_t* table, int32_t max_pages, int64_t pages, int32_t page, int32_t b, int64_t pos);
+
+/*
+ * How ls_packed_prefill counts work, of one sequence: out[0] its row blocks, [1] the 32-key steps of block j, [2] how many blocks take more than x steps, [3] the
+ * bound of all blocks' steps.  And of a call: units[0] the workgroups that it cuts its items for with the workspace that ls_packed_workspace_bytes states (0: it does not),
+ * [1] the items it reckons with; length: steps of a part, for so much work and so many items.
+ */
+int ls_debug_packed_counts(int32_t keys, int32_t queries, int32_t G, int32_t j, int32_t x, int64_t out[4]);
+int ls_debug_packed_units(const ls_shape* shape, int32_t packed, int64_t units[2]);
+int ls_debug_packed_length(int64_t work, int64_t items, int32_t units);
+
+/*
+ * How ls_paged_attend cuts a batch of these lengths (host memory): cuts[b] of each KV head of sequence b; returns the workgroups it launches for
+ * shape->n, *most the parts of a head that it has room for.
+ */
+int ls_debug_paged_cuts(const ls_shape* shape, const int32_t* len, int32_t* cuts, int32_t* most);
+
 #ifdef __cplusplus
 }
 #endif

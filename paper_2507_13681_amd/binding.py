@@ -24,13 +24,23 @@ ENTRY_POINTS = ("ls_workspace_bytes", "ls_create", "ls_destroy", "ls_last_error"
                 "ls_score", "ls_select", "ls_sparse_prefill", "ls_kv_compress", "ls_poll_status")
 # bits of the device status word (ls_poll_status)
 LS_STAT_WALK_TIMEOUT, LS_STAT_S_TRUNCATED, LS_STAT_V_TRUNCATED, LS_STAT_S_RANGE, LS_STAT_V_INVALID = 1, 2, 4, 8, 16
-LS_STAT_MERGE_RANGE = 32
+LS_STAT_MERGE_RANGE, LS_STAT_PAGE_RANGE, LS_STAT_STARTS = 32, 64, 128
+LS_CACHE_BF16, LS_CACHE_E4M3 = 0, 1
 
 
 class LsShape(C.Structure):
     _fields_ = [("B", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32), ("d", C.c_int32),
                 ("n", C.c_int64), ("n_hat", C.c_int64), ("w", C.c_int32), ("dtype", C.c_int32),
                 ("scale", C.c_float)]
+
+
+class LsCache(C.Structure):
+    _fields_ = [("Hkv", C.c_int32), ("d", C.c_int32), ("page", C.c_int32), ("type", C.c_int32), ("pages", C.c_int64),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p)]
+
+
+class LsRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("seq", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
 
 
 class LoopServeError(RuntimeError):
@@ -77,6 +87,34 @@ def load_library():
     lib.ls_decode_attend.argtypes = [vp, sp, i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
     lib.ls_decode_workspace_bytes.restype = C.c_size_t
     lib.ls_decode_workspace_bytes.argtypes = [sp, i32, i32]
+    cp, rp = C.POINTER(LsCache), C.POINTER(LsRows)
+    lib.ls_packed_prefill.restype = C.c_int
+    lib.ls_packed_prefill.argtypes = [vp, sp, rp, rp, rp, vp, vp, rp, vp, vp]
+    lib.ls_packed_workspace_bytes.restype = C.c_size_t
+    lib.ls_packed_workspace_bytes.argtypes = [sp]
+    for move in (lib.ls_cache_write, lib.ls_cache_read):
+        move.restype = C.c_int
+        move.argtypes = [vp, sp, cp, rp, rp, vp, vp, vp, i32, vp, vp]
+    lib.ls_paged_attend.restype = C.c_int
+    lib.ls_paged_attend.argtypes = [vp, sp, cp, vp, vp, i32, vp, vp, vp, vp]
+    lib.ls_paged_workspace_bytes.restype = C.c_size_t
+    lib.ls_paged_workspace_bytes.argtypes = [sp]
+    lib.ls_debug_check_packed.restype = C.c_int
+    lib.ls_debug_check_packed.argtypes = [sp, rp, rp, rp, vp, vp, rp, vp]
+    lib.ls_debug_check_move.restype = C.c_int
+    lib.ls_debug_check_move.argtypes = [sp, cp, rp, rp, vp, vp, vp, i32, vp, i32]
+    lib.ls_debug_check_paged.restype = C.c_int
+    lib.ls_debug_check_paged.argtypes = [sp, cp, vp, vp, i32, vp, vp, vp]
+    lib.ls_debug_page_of.restype = C.c_int
+    lib.ls_debug_page_of.argtypes = [C.POINTER(i32), i32, i64, i32, i32, i64]
+    lib.ls_debug_packed_counts.restype = C.c_int
+    lib.ls_debug_packed_counts.argtypes = [i32, i32, i32, i32, i32, C.POINTER(i64)]
+    lib.ls_debug_packed_units.restype = C.c_int
+    lib.ls_debug_packed_units.argtypes = [sp, i32, C.POINTER(i64)]
+    lib.ls_debug_packed_length.restype = C.c_int
+    lib.ls_debug_packed_length.argtypes = [i64, i64, i32]
+    lib.ls_debug_paged_cuts.restype = C.c_int
+    lib.ls_debug_paged_cuts.argtypes = [sp, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
     lib.ls_debug_copy_compress_score.restype = C.c_int
     lib.ls_debug_copy_compress_score.argtypes = [vp, sp, vp, vp]
     lib.ls_poll_status.restype = C.c_int
@@ -123,6 +161,38 @@ def workspace_bytes(shape: LsShape, budget: int = 0) -> int:
 
 def decode_workspace_bytes(shape: LsShape, cap: int, T: int) -> int:
     return int(load_library().ls_decode_workspace_bytes(C.byref(shape), cap, T))
+
+
+def packed_workspace_bytes(shape: LsShape) -> int:
+    return int(load_library().ls_packed_workspace_bytes(C.byref(shape)))
+
+
+def paged_workspace_bytes(shape: LsShape) -> int:
+    return int(load_library().ls_paged_workspace_bytes(C.byref(shape)))
+
+
+class PagedCache:
+    """A pool of pages (ls_cache): k, v [pages,Hkv,page,d], bf16, or 8-bit e4m3 codes (torch.uint8 or torch.float8_e4m3fn) with
+    k_exp, v_exp [pages,Hkv,page] uint8.  Holds the tensors, which stay the caller's; stored 8-bit values stand for code * 2^(exp - 127)."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        if k.dtype not in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn):
+            raise ValueError("pages are torch.bfloat16, or torch.uint8 or torch.float8_e4m3fn codes")
+        codes = k.dtype != torch.bfloat16
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+            raise ValueError("k and v must be [pages, Hkv, page, d], alike")
+        if codes != (k_exp is not None) or codes != (v_exp is not None):
+            raise ValueError("8-bit pages have exponents, and bf16 pages none")
+        for e in (k_exp, v_exp) if codes else ():
+            if e.dtype != torch.uint8 or e.shape != k.shape[:3]:
+                raise ValueError("exponents must be [pages, Hkv, page] uint8")
+        tensors = [t for t in (k, v, k_exp, v_exp) if t is not None]
+        if not all(t.is_cuda and t.is_contiguous() and t.device == k.device for t in tensors):
+            raise ValueError("pages must be contiguous tensors of one GPU")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.device = k.device.index
+        self.struct = LsCache(k.shape[1], k.shape[3], k.shape[2], LS_CACHE_E4M3 if codes else LS_CACHE_BF16, k.shape[0], k.data_ptr(), v.data_ptr(),
+                              k_exp.data_ptr() if codes else None, v_exp.data_ptr() if codes else None)
 
 
 def _ptr(t):
@@ -212,6 +282,34 @@ class Context:
 
     def ls_decode_attend(self, shape, q, k_c, v_c, cnt, k_t, v_t, out, lse=None):
         rc = self.native.decode_attend(self.hv, shape, q, k_c, v_c, cnt, k_t, v_t, out, lse)
+        if rc:
+            self._check(rc)
+
+    # -- pages and packed sequences.  Rows are [rows, heads, d] where starts say whose they are, [B, heads, rows, d] otherwise, of any strides but
+    # the last; the native marshalling checks types, sizes and devices, since the library sees addresses only
+    def ls_packed_prefill(self, shape, q, k, v, q_starts, k_starts, out, lse=None):
+        rc = self.native.packed_prefill(self.hv, self.device, shape, q, k, v, q_starts, k_starts, out, lse)
+        if rc:
+            self._check(rc)
+
+    def _pages(self, cache):
+        if cache.device != self.device:
+            raise ValueError("the cache is not on the context's GPU")
+        return cache.struct
+
+    def ls_cache_write(self, shape, cache, k, v, table, pos=None, starts=None, count=None):
+        rc = self.native.cache_write(self.hv, self.device, shape, self._pages(cache), k, v, table, pos, starts, count)
+        if rc:
+            self._check(rc)
+
+    def ls_cache_read(self, shape, cache, table, k, v, pos=None, starts=None, count=None):
+        """k, v: where the rows go."""
+        rc = self.native.cache_read(self.hv, self.device, shape, self._pages(cache), k, v, table, pos, starts, count)
+        if rc:
+            self._check(rc)
+
+    def ls_paged_attend(self, shape, cache, q, table, lens, out, lse=None):
+        rc = self.native.paged_attend(self.hv, self.device, shape, self._pages(cache), q, table, lens, out, lse)
         if rc:
             self._check(rc)
 

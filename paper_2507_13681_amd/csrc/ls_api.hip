@@ -17,7 +17,8 @@
 static_assert(ls::TOPB_MAX_LEN == LS_MAX_N, "ls_kv_compress documents LS_MAX_N as its longest cache");
 static_assert(ls::STAT_WALK_TIMEOUT == LS_STAT_WALK_TIMEOUT && ls::STAT_S_TRUNCATED == LS_STAT_S_TRUNCATED &&
               ls::STAT_V_TRUNCATED == LS_STAT_V_TRUNCATED && ls::STAT_S_RANGE == LS_STAT_S_RANGE &&
-              ls::STAT_V_INVALID == LS_STAT_V_INVALID && ls::STAT_MERGE_RANGE == LS_STAT_MERGE_RANGE,
+              ls::STAT_V_INVALID == LS_STAT_V_INVALID && ls::STAT_MERGE_RANGE == LS_STAT_MERGE_RANGE &&
+              ls::STAT_PAGE_RANGE == LS_STAT_PAGE_RANGE && ls::STAT_STARTS == LS_STAT_STARTS,
               "status bits of the kernels and of the header");
 
 struct ls_ctx {
@@ -94,6 +95,8 @@ hipError_t init_device_once(int device) {
     if ((e = ls::init_select_kernels()) != hipSuccess) return e;
     if ((e = ls::init_prefill_kernels()) != hipSuccess) return e;
     if ((e = ls::init_decode_kernels()) != hipSuccess) return e;
+    if ((e = ls::init_paged_kernels()) != hipSuccess) return e;
+    if ((e = ls::init_packed_kernels()) != hipSuccess) return e;
     done[device] = 1;
     return hipSuccess;
 }
@@ -630,6 +633,204 @@ int ls_decode_attend(ls_ctx* c, const ls_shape* s, int32_t cap, int32_t T, const
     return LS_OK;
 }
 
+namespace {
+// The caller's device stays the current one.
+struct OnDevice {
+    int before = -1;
+    bool ok;
+    explicit OnDevice(int device) {
+        ok = hipGetDevice(&before) == hipSuccess && (before == device || hipSetDevice(device) == hipSuccess);
+        if (before == device) before = -1;
+    }
+    ~OnDevice() { if (before >= 0) (void)hipSetDevice(before); }
+};
+
+// What the calls on pages and packed sequences check: each returns what is wrong and sets its status code.
+struct Wrong { int code; const char* what; };
+constexpr Wrong FINE{LS_OK, nullptr};
+
+Wrong check_heads(const ls_shape* s, bool queries) {
+    if (!s) return {LS_ESHAPE, "shape is NULL"};
+    if (s->B <= 0 || s->Hkv <= 0 || (queries && s->Hq <= 0)) return {LS_ESHAPE, queries ? "B, Hq, Hkv must be positive" : "B, Hkv must be positive"};
+    if (queries && s->Hq % s->Hkv) return {LS_ESHAPE, "Hq must be a multiple of Hkv"};
+    if (s->d != 64 && s->d != 128) return {LS_ESHAPE, "d must be 64 or 128"};
+    if (s->dtype != LS_BF16 && s->dtype != LS_F32) return {LS_ESHAPE, "dtype must be LS_BF16 or LS_F32"};
+    if ((int64_t)s->B * (queries ? s->Hq : s->Hkv) > 65535) return {LS_ESHAPE, queries ? "B * Hq too large" : "B * Hkv too large"};
+    return FINE;
+}
+constexpr int64_t MOST_ROWS = 2147483000LL;
+
+// counts: sequences (1 where they are packed), rows, heads; `written`: no two rows may share an element
+Wrong check_rows(const ls_rows* r, int dtype, int d, int64_t seqs, int64_t rows, int64_t heads, bool written) {
+    if (!r || !r->data) return {LS_EINVAL, "NULL tensor"};
+    const int64_t unit = dtype == LS_BF16 ? 8 : 4;
+    if (!aligned16(r->data) || r->seq % unit || r->row % unit || r->head % unit) return {LS_EINVAL, "rows must begin at multiples of 16 bytes"};
+    std::array<std::array<int64_t, 2>, 3> dim = {{{r->seq, seqs}, {r->row, rows}, {r->head, heads}}};
+    std::sort(dim.begin(), dim.end());
+    __int128 reach = d;                                    // elements from the first one on that the dimensions so far touch
+    for (const auto& x : dim) {
+        if (x[0] < 0) return {LS_ESHAPE, "strides must not be negative"};
+        if (x[1] <= 1) continue;
+        if (written && x[0] < reach) return {LS_ESHAPE, "rows of an output overlap"};
+        reach += (__int128)x[0] * (x[1] - 1);
+        if (reach > ((__int128)1 << 60)) return {LS_ESHAPE, "strides are too large"};
+    }
+    return FINE;
+}
+Wrong check_cache(const ls_cache* c, const ls_shape* s, const int32_t* table, int32_t max_pages) {
+    if (!c) return {LS_EINVAL, "cache is NULL"};
+    if (c->type != LS_CACHE_BF16 && c->type != LS_CACHE_E4M3) return {LS_EINVAL, "cache type must be LS_CACHE_BF16 or LS_CACHE_E4M3"};
+    if (c->Hkv != s->Hkv || c->d != s->d) return {LS_ESHAPE, "Hkv and d of the cache and of the shape differ"};
+    if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1))) return {LS_ESHAPE, "page must be 16, 32, 64, 128 or 256"};
+    if (c->pages < 1 || c->pages > 2147483647LL) return {LS_ESHAPE, "need 1 <= pages < 2^31"};
+    if (max_pages < 1) return {LS_ESHAPE, "max_pages must be positive"};
+    const bool e = c->type == LS_CACHE_E4M3;
+    if (!c->k || !c->v || !table || (e && (!c->k_exp || !c->v_exp))) return {LS_EINVAL, "NULL tensor"};
+    if (!aligned16(c->k) || !aligned16(c->v) || (e && (!aligned16(c->k_exp) || !aligned16(c->v_exp)))) return {LS_EINVAL, "misaligned cache"};
+    return FINE;
+}
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+ls::CacheArgs cache_args(const ls_cache* c, const int32_t* table, int32_t max_pages) {
+    ls::CacheArgs a{};
+    a.k = static_cast<unsigned char*>(c->k); a.v = static_cast<unsigned char*>(c->v); a.kx = c->k_exp; a.vx = c->v_exp;
+    a.table = table; a.max_pages = max_pages; a.pages = (uint32_t)c->pages; a.Hkv = c->Hkv; a.page_log = __builtin_ctz((unsigned)c->page);
+    return a;
+}
+ls::RowArgs row_args(const ls_rows* r) { return {static_cast<unsigned char*>(r->data), r->seq, r->row, r->head}; }
+
+Wrong check_move(const ls_shape* s, const ls_cache* cache, const ls_rows* k, const ls_rows* v, const int32_t* starts, const int32_t* count,
+                 const int32_t* table, int32_t max_pages, const int32_t* pos, bool write) {
+    Wrong w = check_heads(s, false);
+    if (w.code) return w;
+    const int64_t seqs = starts ? 1 : s->B;
+    if (s->n_hat < 1 || s->n_hat > MOST_ROWS || seqs * s->n_hat > MOST_ROWS) return {LS_ESHAPE, "rows out of range"};
+    if (starts && count) return {LS_EINVAL, "count goes without starts only"};
+    if (!aligned4(starts) || !aligned4(count) || !aligned4(table) || !aligned4(pos)) return {LS_EINVAL, "misaligned index tensor"};
+    if ((w = check_cache(cache, s, table, max_pages)).code) return w;
+    if ((w = check_rows(k, s->dtype, s->d, seqs, s->n_hat, s->Hkv, !write)).code) return w;
+    return check_rows(v, s->dtype, s->d, seqs, s->n_hat, s->Hkv, !write);
+}
+int cache_move(ls_ctx* c, const char* who, bool write, const ls_shape* s, const ls_cache* cache, const ls_rows* k, const ls_rows* v,
+               const int32_t* starts, const int32_t* count, const int32_t* table, int32_t max_pages, const int32_t* pos, void* stream) {
+    if (!c) return LS_EINVAL;
+    if (const Wrong w = check_move(s, cache, k, v, starts, count, table, max_pages, pos, write); w.code) return fail(c, w.code, "%s: %s", who, w.what);
+    ls::MoveArgs a{};
+    a.cache = cache_args(cache, table, max_pages); a.k = row_args(k); a.v = row_args(v);
+    a.starts = starts; a.count = count; a.pos = pos; a.B = s->B; a.n_hat = (int)s->n_hat; a.status = c->status;
+    const OnDevice on(c->device);
+    if (!on.ok) return fail(c, LS_EHIP, "%s: hipSetDevice failed", who);
+    const hipError_t e = ls::run_move(a, write, s->dtype, cache->type, s->d, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(c, LS_EHIP, "%s: %s", who, hipGetErrorString(e));
+    return LS_OK;
+}
+
+Wrong check_paged_shape(const ls_shape* s) {
+    const Wrong w = check_heads(s, true);
+    if (w.code) return w;
+    if (s->dtype != LS_BF16) return {LS_ESHAPE, "dtype must be LS_BF16"};
+    if (s->Hq / s->Hkv > 32) return {LS_ESHAPE, "at most 32 query heads per KV head"};
+    if (s->n < 1 || s->n > MOST_ROWS) return {LS_ESHAPE, "n out of range"};
+    return FINE;
+}
+Wrong check_paged(const ls_shape* s, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages, const int32_t* len, const void* out,
+                  const float* lse) {
+    Wrong w = check_paged_shape(s);
+    if (w.code || (w = check_cache(cache, s, table, max_pages)).code) return w;
+    if (!q || !len || !out) return {LS_EINVAL, "NULL tensor"};
+    if (!aligned16(q) || !aligned16(out) || !aligned4(table) || !aligned4(len) || !aligned4(lse)) return {LS_EINVAL, "misaligned tensor"};
+    return FINE;
+}
+Wrong check_packed_shape(const ls_shape* s) {
+    const Wrong w = check_heads(s, true);
+    if (w.code) return w;
+    if (s->n < 1 || s->n > MOST_ROWS || s->n_hat < 1 || s->n_hat * (s->Hq / s->Hkv) > MOST_ROWS) return {LS_ESHAPE, "n or n_hat out of range"};
+    return FINE;
+}
+Wrong check_packed(const ls_shape* s, const ls_rows* q, const ls_rows* k, const ls_rows* v, const int32_t* q_starts, const int32_t* k_starts,
+                   const ls_rows* out, const float* lse) {
+    Wrong w = check_packed_shape(s);
+    if (w.code) return w;
+    if (!q_starts != !k_starts) return {LS_EINVAL, "q_starts and k_starts go together"};
+    if (!aligned4(q_starts) || !aligned4(k_starts) || !aligned4(lse)) return {LS_EINVAL, "misaligned tensor"};
+    const int64_t seqs = q_starts ? 1 : s->B;
+    if ((w = check_rows(q, s->dtype, s->d, seqs, s->n_hat, s->Hq, false)).code || (w = check_rows(out, s->dtype, s->d, seqs, s->n_hat, s->Hq, true)).code ||
+        (w = check_rows(k, s->dtype, s->d, seqs, s->n, s->Hkv, false)).code || (w = check_rows(v, s->dtype, s->d, seqs, s->n, s->Hkv, false)).code) return w;
+    const int64_t reach = 32 * (s->dtype == LS_BF16 ? 2 : 4);                // (a step's rows are reached by 32-bit offsets)
+    if (k->row > (1LL << 31) / reach - 1 || v->row > (1LL << 31) / reach - 1) return {LS_ESHAPE, "rows of k or v are too far apart"};
+    return FINE;
+}
+// Items are cut into as many parts as there is room for their results.
+int packed_units(const ls_shape* s, bool packed, size_t room) {
+    const int G = s->Hq / s->Hkv;
+    const int64_t items = ls::packed_items(s->B, s->n_hat, s->Hkv, G, packed);
+    const int64_t slots = (int64_t)(room / (ls::prefill_slot_bytes(s->d))), most = s->B > ls::PACKED_SORTED ? 0 : ls::packed_units(items, s->dtype, s->d);
+    const int64_t units = (slots < most ? slots : most) / 8 * 8;
+    return units > items ? (int)units : 0;
+}
+size_t paged_bytes(const ls_shape* s) {
+    if (ls::paged_most_cuts(s->Hkv, s->n) == 1) return 0;
+    return up((size_t)ls::paged_units(s->B, s->Hkv, s->n) * (s->Hq / s->Hkv) * ls::decode_part_floats(s->d) * 4);
+}
+}  // namespace
+
+int ls_cache_write(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const ls_rows* k, const ls_rows* v, const int32_t* starts,
+                   const int32_t* count, const int32_t* table, int32_t max_pages, const int32_t* pos, void* stream) {
+    return cache_move(c, "ls_cache_write", true, s, cache, k, v, starts, count, table, max_pages, pos, stream);
+}
+
+int ls_cache_read(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const ls_rows* k, const ls_rows* v, const int32_t* starts,
+                  const int32_t* count, const int32_t* table, int32_t max_pages, const int32_t* pos, void* stream) {
+    return cache_move(c, "ls_cache_read", false, s, cache, k, v, starts, count, table, max_pages, pos, stream);
+}
+
+size_t ls_packed_workspace_bytes(const ls_shape* s) {
+    if (check_packed_shape(s).code) return 0;
+    const size_t room = (size_t)1 << 40;                   // (with starts there may be more items, and so no need of parts)
+    const int units = std::max(packed_units(s, true, room), packed_units(s, false, room));
+    return up((size_t)units * ls::prefill_slot_bytes(s->d)) + ALIGN;
+}
+
+int ls_packed_prefill(ls_ctx* c, const ls_shape* s, const ls_rows* q, const ls_rows* k, const ls_rows* v, const int32_t* q_starts,
+                      const int32_t* k_starts, const ls_rows* out, float* lse, void* stream) {
+    if (!c) return LS_EINVAL;
+    if (const Wrong w = check_packed(s, q, k, v, q_starts, k_starts, out, lse); w.code) return fail(c, w.code, "ls_packed_prefill: %s", w.what);
+    ls::PackedArgs a{};
+    a.q = row_args(q); a.k = row_args(k); a.v = row_args(v); a.out = row_args(out); a.lse = lse; a.q_starts = q_starts; a.k_starts = k_starts;
+    a.B = s->B; a.Hq = s->Hq; a.Hkv = s->Hkv; a.G = s->Hq / s->Hkv; a.n = (int)s->n; a.n_hat = (int)s->n_hat;
+    a.scale_log2e = scale_log2e(s); a.status = c->status;
+    a.units = packed_units(s, q_starts != nullptr, c->ws_bytes);
+    a.part_o = reinterpret_cast<float*>(c->ws);
+    a.part_ml = a.part_o + (size_t)a.units * ls::PACKED_ROWS * s->d;
+    const OnDevice on(c->device);
+    if (!on.ok) return fail(c, LS_EHIP, "ls_packed_prefill: hipSetDevice failed");
+    const hipError_t e = ls::run_packed(a, s->dtype, s->d, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(c, LS_EHIP, "ls_packed_prefill: %s", hipGetErrorString(e));
+    return LS_OK;
+}
+
+size_t ls_paged_workspace_bytes(const ls_shape* s) { return check_paged_shape(s).code ? 0 : paged_bytes(s) + ALIGN; }
+
+int ls_paged_attend(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages,
+                    const int32_t* len, void* out, float* lse, void* stream) {
+    if (!c) return LS_EINVAL;
+    if (const Wrong w = check_paged(s, cache, q, table, max_pages, len, out, lse); w.code) return fail(c, w.code, "ls_paged_attend: %s", w.what);
+    if (paged_bytes(s) > c->ws_bytes) return fail(c, LS_EWORKSPACE, "ls_paged_attend: workspace of %zu bytes is too small", c->ws_bytes);
+    ls::PagedArgs a{};
+    a.cache = cache_args(cache, table, max_pages);
+    a.q = q; a.len = len; a.out = out; a.lse = lse; a.part = reinterpret_cast<float*>(c->ws);
+    a.B = s->B; a.Hq = s->Hq; a.Hkv = s->Hkv; a.G = s->Hq / s->Hkv; a.most = s->n; a.scale_log2e = scale_log2e(s); a.status = c->status;
+    const bool counts = ls::paged_most_cuts(s->Hkv, s->n) > 1;
+    a.done = decode_set(c, c->decode_calls);
+    a.done_clear = decode_set(c, c->decode_calls + 2);
+    a.clear_heads = !counts ? 0 : c->decode_heads > s->B * s->Hkv ? c->decode_heads : s->B * s->Hkv;
+    const OnDevice on(c->device);
+    if (!on.ok) return fail(c, LS_EHIP, "ls_paged_attend: hipSetDevice failed");
+    const hipError_t e = ls::run_paged(a, cache->type, s->d, ls::paged_units(s->B, s->Hkv, s->n), static_cast<hipStream_t>(stream));
+    if (counts) { ++c->decode_calls; c->decode_heads = a.clear_heads; }
+    if (e != hipSuccess) return fail(c, LS_EHIP, "ls_paged_attend: %s", hipGetErrorString(e));
+    return LS_OK;
+}
+
 int ls_profile_enable(ls_ctx* c, int on) {
     if (!c) return LS_EINVAL;
     (void)hipSetDevice(c->device);
@@ -789,6 +990,45 @@ int ls_debug_score_route(const ls_shape* s, int32_t mode, int32_t positions, int
         begins[x] = key < s->n ? key : s->n;
     }
     return LS_OK;
+}
+
+int ls_debug_check_packed(const ls_shape* s, const ls_rows* q, const ls_rows* k, const ls_rows* v, const int32_t* q_starts, const int32_t* k_starts,
+                          const ls_rows* out, const float* lse) {
+    return check_packed(s, q, k, v, q_starts, k_starts, out, lse).code;
+}
+int ls_debug_check_move(const ls_shape* s, const ls_cache* cache, const ls_rows* k, const ls_rows* v, const int32_t* starts, const int32_t* count,
+                        const int32_t* table, int32_t max_pages, const int32_t* pos, int32_t write) {
+    return check_move(s, cache, k, v, starts, count, table, max_pages, pos, write != 0).code;
+}
+int ls_debug_check_paged(const ls_shape* s, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages, const int32_t* len,
+                         const void* out, const float* lse) {
+    return check_paged(s, cache, q, table, max_pages, len, out, lse).code;
+}
+int ls_debug_page_of(const int32_t* table, int32_t max_pages, int64_t pages, int32_t page, int32_t b, int64_t pos) {
+    ls::CacheArgs a{};
+    a.table = table; a.max_pages = max_pages; a.pages = (uint32_t)pages; a.page_log = __builtin_ctz((unsigned)page);
+    return ls::page_of(a, b, pos);
+}
+int ls_debug_packed_counts(int32_t keys, int32_t queries, int32_t G, int32_t j, int32_t x, int64_t out[4]) {
+    const ls::PackedSeq s{keys, queries};
+    out[0] = ls::packed_blocks(queries, G); out[1] = ls::packed_steps(s, G, j); out[2] = ls::packed_longer(s, G, x); out[3] = ls::packed_work(s, G);
+    return LS_OK;
+}
+int ls_debug_packed_units(const ls_shape* s, int32_t packed, int64_t units[2]) {
+    if (const Wrong w = check_packed_shape(s); w.code) return w.code;
+    units[0] = packed_units(s, packed != 0, ls_packed_workspace_bytes(s));
+    units[1] = ls::packed_items(s->B, s->n_hat, s->Hkv, s->Hq / s->Hkv, packed != 0);
+    return LS_OK;
+}
+int ls_debug_packed_length(int64_t work, int64_t items, int32_t units) { return ls::packed_length(work, items, units); }
+int ls_debug_paged_cuts(const ls_shape* s, const int32_t* len, int32_t* cuts, int32_t* most) {
+    if (const Wrong w = check_paged_shape(s); w.code) return w.code;
+    int64_t tiles = 0;
+    for (int b = 0; b < s->B; ++b) tiles += (len[b] + ls::PAGED_TILE - 1) / ls::PAGED_TILE;
+    const int length = ls::paged_length(tiles, s->Hkv);
+    for (int b = 0; b < s->B; ++b) cuts[b] = ls::paged_cuts((len[b] + ls::PAGED_TILE - 1) / ls::PAGED_TILE, length);
+    *most = ls::paged_most_cuts(s->Hkv, s->n);
+    return ls::paged_units(s->B, s->Hkv, s->n);
 }
 
 /* Debug / test hook: the group-summed retention score of the last ls_kv_compress call on this

@@ -169,9 +169,110 @@ struct DecodeArgs {
     float scale_log2e;
 };
 
+// A paged cache (ls_cache)
+struct CacheArgs {
+    unsigned char *k, *v;     // [pages][Hkv][page][d] bf16 or e4m3
+    uint8_t *kx, *vx;         // [pages][Hkv][page] e4m3: exponents
+    const int32_t* table;     // [B][max_pages]
+    int max_pages;
+    uint32_t pages;
+    int Hkv, page_log;        // a page holds 2^page_log positions
+};
+// Rows of a caller's tensor (ls_rows)
+struct RowArgs {
+    unsigned char* data;
+    int64_t seq, row, head;   // strides, elements
+};
+// The page of position p of sequence b as the table has it, or -1: that position is nowhere.
+__host__ __device__ inline int page_of(const CacheArgs& c, int b, int64_t p) {
+    const int64_t at = p >> c.page_log;
+    if (p < 0 || at >= c.max_pages) return -1;
+    const int32_t id = c.table[(int64_t)b * c.max_pages + at];
+    return (uint32_t)id < c.pages ? id : -1;
+}
+// Rows a .. e - 1 of `rows`, as a sequence's starts say: whether they are any
+__host__ __device__ inline bool starts_ok(int32_t a, int32_t e, int64_t rows) { return a >= 0 && e >= a && e <= rows; }
+
+struct MoveArgs {
+    CacheArgs cache;
+    RowArgs k, v;
+    const int32_t *starts, *count, *pos;       // as ls_cache_write has them
+    int B, n_hat;
+    int heads;                // KV heads of a workgroup
+    int32_t* status;
+};
+
+// ls_paged_attend.  A unit of work is up to `length` 32-key tiles of one KV head of one sequence, and a workgroup has one.  Which one
+// follows from the lengths, which only the device knows: a head's tiles are cut into paged_cuts parts.
+constexpr int PAGED_TILE = 32;               // keys
+constexpr int PAGED_WORKERS = 256;           // units that the work of all heads is cut into, beside the one that each has at least
+__host__ __device__ inline int paged_length(int64_t tiles, int heads) {             // of a unit; tiles: of all sequences, each with `heads` KV heads
+    const int64_t each = (tiles * heads + PAGED_WORKERS - 1) / PAGED_WORKERS;
+    return each < 4 ? 4 : each < 1 << 30 ? (int)each : 1 << 30;
+}
+__host__ __device__ inline int paged_cuts(int tiles, int length) { return tiles <= 18 ? 1 : (tiles + length - 1) / length; }
+struct PagedArgs {
+    CacheArgs cache;
+    const void* q;            // [B][Hq][d]
+    const int32_t* len;       // [B]
+    void* out;                // [B][Hq][d]
+    float* lse;               // [B][Hq] or NULL
+    float* part;              // [units][G][d + 4] output, reference, normaliser of each part of a head
+    uint32_t* done;           // [B*Hkv] parts finished; zero between calls
+    uint32_t* done_clear;     // [clear_heads] the counters of the call after the next, cleared here
+    int clear_heads;
+    int B, Hq, Hkv, G;
+    int64_t most;             // no sequence is longer
+    float scale_log2e;
+    int32_t* status;
+};
+
+// ls_packed_prefill.  An item is a block of 128 rows of one KV head of one sequence, where a "row" is one of the G query heads of one query: row r is head r % G of query
+// r / G.  Items go by how many 32-key steps they take, the longest first; where there are few of them they are cut into parts of `length` steps.
+constexpr int PACKED_ROWS = 128, PACKED_KEYS = 32;
+struct PackedSeq { int keys, queries; };
+__host__ __device__ inline int packed_blocks(int queries, int G) { return (int)(((int64_t)queries * G + PACKED_ROWS - 1) / PACKED_ROWS); }
+// steps that block j of a sequence takes: those up to the last key that its last row sees
+__host__ __device__ inline int packed_steps(const PackedSeq& s, int G, int j) {
+    const int64_t rows = (int64_t)s.queries * G, end = (int64_t)PACKED_ROWS * (j + 1) < rows ? (int64_t)PACKED_ROWS * (j + 1) : rows;
+    const int64_t seen = (int64_t)s.keys - s.queries + (end - 1) / G + 1;
+    return seen > 0 ? (int)((seen + PACKED_KEYS - 1) / PACKED_KEYS) : 0;
+}
+// blocks of a sequence that take more than x steps: its last ones.  (The last row sees query y or one after it, y = 32 x - keys + queries, if
+// the block ends behind row y G.)
+__host__ __device__ inline int packed_longer(const PackedSeq& s, int G, int x) {
+    const int blocks = packed_blocks(s.queries, G);
+    if (x < 0) return blocks;
+    const int64_t y = (int64_t)PACKED_KEYS * x - s.keys + s.queries;
+    if (y >= s.queries) return 0;
+    return y <= 0 ? blocks : blocks - (int)(y * G / PACKED_ROWS);
+}
+// no less than the steps of all its blocks together
+__host__ __device__ inline int64_t packed_work(const PackedSeq& s, int G) {
+    const int64_t blocks = packed_blocks(s.queries, G), before = s.keys > s.queries ? s.keys - s.queries : 0;
+    return blocks * (before / PACKED_KEYS + 4) + PACKED_ROWS / PACKED_KEYS * (blocks * (blocks + 1) / 2) / G;
+}
+constexpr int PACKED_SORTED = 64;            // with more sequences items go by sequence, whole
+constexpr int PACKED_SHORTEST = 8;           // steps of a part, at least
+__host__ __device__ inline int packed_length(int64_t work, int64_t items, int units) {           // work, items: of all KV heads; units > items
+    const int64_t each = (work + (units - items) - 1) / (units - items);
+    return each < PACKED_SHORTEST ? PACKED_SHORTEST : each < 1 << 30 ? (int)each : 1 << 30;
+}
+struct PackedArgs {
+    RowArgs q, k, v, out;
+    const int32_t *q_starts, *k_starts;
+    float* lse;
+    int B, Hq, Hkv, G;
+    int n, n_hat;
+    float scale_log2e;
+    int units;                // workgroups, if items are cut (else 0)
+    float *part_o, *part_ml;  // [units][128][d] accumulators in lane order, [units][128][2] reference and normaliser
+    int32_t* status;
+};
+
 // status bits (mirrors of LS_STAT_* in loopserve.h)
 constexpr int STAT_WALK_TIMEOUT = 1, STAT_S_TRUNCATED = 2, STAT_V_TRUNCATED = 4, STAT_S_RANGE = 8, STAT_V_INVALID = 16,
-              STAT_MERGE_RANGE = 32;
+              STAT_MERGE_RANGE = 32, STAT_PAGE_RANGE = 64, STAT_STARTS = 128;
 constexpr int WALK_SPIN_DEFAULT = 1 << 22;   // never reached in practice (about a second of polling)
 
 // Lets a kernel use all of a compute unit's LDS (160 KB, less what the kernel declares statically) as
@@ -191,6 +292,16 @@ hipError_t init_select_kernels();
 hipError_t init_prefill_kernels();
 hipError_t init_decode_kernels();
 
+hipError_t init_paged_kernels();
+
+hipError_t init_packed_kernels();
+hipError_t run_packed(const PackedArgs& a, int dtype, int d, hipStream_t st);
+int packed_units(int64_t items, int dtype, int d);                   // workgroups that so many items are cut for (0: they are not)
+int64_t packed_items(int B, int64_t n_hat, int Hkv, int G, bool packed);       // no fewer than there are
+hipError_t run_move(const MoveArgs& a, bool write, int dtype, int type, int d, hipStream_t st);
+hipError_t run_paged(const PagedArgs& a, int type, int d, int units, hipStream_t st);
+int paged_units(int B, int Hkv, int64_t most);                       // workgroups that sequences of up to so many keys take
+int paged_most_cuts(int Hkv, int64_t most);                          // ... and parts of a head
 hipError_t run_score(const ScoreArgs& a, int dtype, int d, int mode, hipStream_t st);
 hipError_t run_decode(const DecodeArgs& a, int d, hipStream_t st);
 size_t decode_smem_bytes(int d, int G, int nsplit);
