@@ -768,7 +768,7 @@ int packed_units(const ls_shape* s, bool packed, size_t room) {
     return units > items ? (int)units : 0;
 }
 size_t paged_bytes(const ls_shape* s) {
-    if (ls::paged_most_cuts(s->Hkv, s->n) == 1) return 0;
+    if (ls::paged_most_cuts(s->B, s->Hkv, s->n) == 1) return 0;
     return up((size_t)ls::paged_units(s->B, s->Hkv, s->n) * (s->Hq / s->Hkv) * ls::decode_part_floats(s->d) * 4);
 }
 }  // namespace
@@ -819,8 +819,8 @@ int ls_paged_attend(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const v
     a.cache = cache_args(cache, table, max_pages);
     a.q = q; a.len = len; a.out = out; a.lse = lse; a.part = reinterpret_cast<float*>(c->ws);
     a.B = s->B; a.Hq = s->Hq; a.Hkv = s->Hkv; a.G = s->Hq / s->Hkv; a.most = s->n; a.scale_log2e = scale_log2e(s); a.status = c->status;
-    const bool counts = ls::paged_most_cuts(s->Hkv, s->n) > 1;
-    a.done = decode_set(c, c->decode_calls);
+    const bool joins = ls::paged_joins(s->B, s->Hkv, a.G, s->n), counts = joins && ls::paged_most_cuts(s->B, s->Hkv, s->n) > 1;
+    a.done = joins ? decode_set(c, c->decode_calls) : nullptr;
     a.done_clear = decode_set(c, c->decode_calls + 2);
     a.clear_heads = !counts ? 0 : c->decode_heads > s->B * s->Hkv ? c->decode_heads : s->B * s->Hkv;
     const OnDevice on(c->device);
@@ -1025,9 +1025,14 @@ int ls_debug_paged_cuts(const ls_shape* s, const int32_t* len, int32_t* cuts, in
     if (const Wrong w = check_paged_shape(s); w.code) return w.code;
     int64_t tiles = 0;
     for (int b = 0; b < s->B; ++b) tiles += (len[b] + ls::PAGED_TILE - 1) / ls::PAGED_TILE;
-    const int length = ls::paged_length(tiles, s->Hkv);
-    for (int b = 0; b < s->B; ++b) cuts[b] = ls::paged_cuts((len[b] + ls::PAGED_TILE - 1) / ls::PAGED_TILE, length);
-    *most = ls::paged_most_cuts(s->Hkv, s->n);
+    ls::PagedLength l(tiles * s->Hkv, (int64_t)s->B * s->Hkv);
+    if (s->B > 64) l.length = l.enough;
+    int64_t units;
+    do {
+        units = 0;
+        for (int b = 0; b < s->B; ++b) units += (int64_t)s->Hkv * (cuts[b] = ls::paged_cuts((len[b] + ls::PAGED_TILE - 1) / ls::PAGED_TILE, l.length));
+    } while (!l.accepts(units));
+    *most = ls::paged_most_cuts(s->B, s->Hkv, s->n);
     return ls::paged_units(s->B, s->Hkv, s->n);
 }
 

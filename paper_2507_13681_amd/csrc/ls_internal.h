@@ -202,15 +202,42 @@ struct MoveArgs {
     int32_t* status;
 };
 
-// ls_paged_attend.  A unit of work is up to `length` 32-key tiles of one KV head of one sequence, and a workgroup has one.  Which one
-// follows from the lengths, which only the device knows: a head's tiles are cut into paged_cuts parts.
+// ls_paged_attend.  A unit of work is a part of the 32-key tiles of one KV head of one sequence, and a workgroup has one.  Which one follows from the lengths, which only the device
+// knows.
 constexpr int PAGED_TILE = 32;               // keys
-constexpr int PAGED_WORKERS = 256;           // units that the work of all heads is cut into, beside the one that each has at least
-__host__ __device__ inline int paged_length(int64_t tiles, int heads) {             // of a unit; tiles: of all sequences, each with `heads` KV heads
-    const int64_t each = (tiles * heads + PAGED_WORKERS - 1) / PAGED_WORKERS;
-    return each < 4 ? 4 : each < 1 << 30 ? (int)each : 1 << 30;
-}
-__host__ __device__ inline int paged_cuts(int tiles, int length) { return tiles <= 18 ? 1 : (tiles + length - 1) / length; }
+// Few heads go in as many parts as there are compute units, which have a workgroup each; more heads, whose lengths may differ, in twice as many at most, two workgroups to a unit: what is
+// left over at the ends is shorter then, but a part more is a result more to put together.  256 parts / 512, us: four caches of 16384, 8 KV heads, e4m3 27.2 / 29.6, one of 131072, bf16 99 / 105; 13 caches of
+// 1 to 131072 112 / 106, 64 of 100 to 20000 115 / 104.  Parts are as short as lets all of them run at once (four caches of 500 to 60000, against the work by 256 and what the heads begin more in a
+// second round: 53 / 36 us, eight of 1000 to 30000 59 / 44).
+constexpr int PAGED_ALONE = 64;              // heads up to which a workgroup has its compute unit for itself
+__host__ __device__ inline int paged_slots(int64_t heads) { return heads <= PAGED_ALONE ? 256 : 512; }
+__host__ __device__ inline bool paged_at_once(int64_t heads) { return heads * 4 <= paged_slots(heads) * 3; }
+// Tiles that a head is not cut for, two a wave: 17 tiles whole / in parts 9.5 / 8.6 us, 10 tiles 6.7 / 8.1
+constexpr int PAGED_WHOLE = 16;
+constexpr int PAGED_SHORTEST = 4, PAGED_SHORTEST_MANY = 32;                          // tiles of a part at least; of that many heads
+__host__ __device__ inline int paged_cuts(int tiles, int length) { return tiles <= PAGED_WHOLE ? 1 : (int)(((uint32_t)tiles + (uint32_t)length - 1) / (uint32_t)length); }
+// Tiles of a part of a call, of so many tiles in all: what `length` makes of them is counted until it is accepted
+struct PagedLength {
+    int length, enough, slots, tries;        // enough: it will do, whatever the sequences are
+    bool sorts;                              // not all parts run at once: the longest first
+    __host__ __device__ PagedLength(int64_t tiles, int64_t heads) : slots(paged_slots(heads)), tries(0) {
+        const bool at_once = paged_at_once(heads);
+        sorts = !at_once;
+        auto least = [&](int64_t parts) {
+            const int64_t each = (tiles + parts - 1) / parts, from = at_once ? PAGED_SHORTEST : PAGED_SHORTEST_MANY;
+            return each < from ? (int)from : each < 1 << 30 ? (int)each : 1 << 30;
+        };
+        length = least(slots);
+        enough = at_once ? least(slots - heads) : length;      // (a part begun in each head)
+    }
+    __host__ __device__ bool accepts(int64_t units) {
+        if (units <= slots || length >= enough) return true;
+        const int64_t more = length * (units - slots) / slots / 2;
+        length += more > 1 ? (int)more : 1;
+        if (length > enough || ++tries == 4) length = enough;
+        return false;
+    }
+};
 struct PagedArgs {
     CacheArgs cache;
     const void* q;            // [B][Hq][d]
@@ -218,7 +245,7 @@ struct PagedArgs {
     void* out;                // [B][Hq][d]
     float* lse;               // [B][Hq] or NULL
     float* part;              // [units][G][d + 4] output, reference, normaliser of each part of a head
-    uint32_t* done;           // [B*Hkv] parts finished; zero between calls
+    uint32_t* done;           // [B*Hkv] parts finished; zero between calls.  Null: paged_join_kernel puts the parts together
     uint32_t* done_clear;     // [clear_heads] the counters of the call after the next, cleared here
     int clear_heads;
     int B, Hq, Hkv, G;
@@ -301,7 +328,8 @@ int64_t packed_items(int B, int64_t n_hat, int Hkv, int G, bool packed);       /
 hipError_t run_move(const MoveArgs& a, bool write, int dtype, int type, int d, hipStream_t st);
 hipError_t run_paged(const PagedArgs& a, int type, int d, int units, hipStream_t st);
 int paged_units(int B, int Hkv, int64_t most);                       // workgroups that sequences of up to so many keys take
-int paged_most_cuts(int Hkv, int64_t most);                          // ... and parts of a head
+bool paged_joins(int B, int Hkv, int G, int64_t most);                      // the kernel puts parts together itself
+int paged_most_cuts(int B, int Hkv, int64_t most);                   // ... and parts of a head
 hipError_t run_score(const ScoreArgs& a, int dtype, int d, int mode, hipStream_t st);
 hipError_t run_decode(const DecodeArgs& a, int d, hipStream_t st);
 size_t decode_smem_bytes(int d, int G, int nsplit);

@@ -4,12 +4,14 @@
 // The step reads every K and V row once and does 4 d FLOP per (query head, key): it is bound by HBM bandwidth, at small sizes by latency.
 // The query heads of a KV head are the columns of 16x16x32 products (NH blocks of 16), so that the rows are read once for all of them.
 //   Work.  What there is to do follows from the lengths, which only the device knows: every wave adds them up, cuts each KV head's 32-key tiles into parts of about
-//   equal length and finds the part that its workgroup has (paged_length, paged_cuts), so a batch of one long and many short sequences fills the chip as one of equals does.
+//   equal length (PagedLength) and finds the part that its workgroup has, so a batch of one long and many short sequences fills the chip as one of equals does.
 //   A part.  The waves of a workgroup take its tiles in turn.  S^T = K Q^T with K fragments straight from global memory, online softmax per head in a lane,
 //   P -> bf16, O^T += V^T P^T with the V^T fragments read transposed from a wave-private, swizzled LDS copy of the 32 V rows that a global -> LDS transfer filled.
 //   e4m3: K codes become bf16 with their row's power of two in one instruction for two of them, exactly; V codes come through the 8-bit transpose read and
 //   become bf16 as they are, and their rows' powers go into the probabilities, exactly too.
-//   The waves' partial results are merged through LDS; where a head is in parts, the workgroup that finishes it last merges those.
+//   The waves' partial results are merged through LDS; where a head is in parts, the workgroup that finishes it last merges those, or, of many parts and query heads, a launch more does.
+// One token of one sequence, 8 KV heads of 128, 32 query heads, us: 300 keys e4m3 7.1 (an empty launch is 4.7), 519 bf16 8.8, 131072 bf16 97 (5.5 TB/s), e4m3 48; 64 query heads, four caches of
+// 16384, e4m3 27 (5.0 TB/s).
 // Pages.  A page holds a multiple of 16 positions, so that each half of a tile lies in one: lane l of a wave keeps the page of half l of its next 64, and a
 // tile's two are lane reads.  What lies behind the length in the last page is read with it, and left out by selects; a half in no page at all is read from page 0 and left out.
 #include "ls_device.h"
@@ -18,6 +20,9 @@
 namespace ls {
 
 constexpr int PG_WAVES = 8, PG_THREADS = 64 * PG_WAVES, PG_BATCH = 8;
+// Parts x query heads that the last workgroup of a head puts together itself; it reads their results alone, 30 to 50 KB a us.  Itself / by a launch more, us: 32 x 4 97.0 / 96.5, 8 x 8 26.7 / 28.0,
+// 17 x 8 10.8 / 12.3, 128 x 8 15.4 / 11.9, 128 x 32 53 / 13, 256 x 32 176 / 22.
+constexpr int PAGED_JOIN = 320;
 
 template <int D, bool E4M3>
 struct PagedCfg {
@@ -46,8 +51,88 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t lo, uint32_t hi, float f) {  
 }
 __device__ __forceinline__ float power_of_byte(uint32_t w, int i) { return __builtin_bit_cast(float, (w >> (8 * i) & 0xFFu) << 23); }
 
+__device__ __forceinline__ int paged_tiles(int n) { return (int)(((uint32_t)n + PAGED_TILE - 1) / PAGED_TILE); }
+
+// The units of a call, as the lengths have them: a lane has a sequence of the 64 at hand.  Of those the ones with the longest parts come first, so that the short ones
+// fill what these leave.
+struct PagedUnits {
+    int b, kvh, cut, cuts, n; // sequence, KV head, part, parts of the head, length
+    int base;                 // first unit of the head
+    int64_t most;             // no sequence is longer
+    __device__ int length_of(const PagedArgs& a, int i) const {                // of sequence i, as far as it can be
+        const int x = i < a.B ? a.len[i] : 0;
+        return x < 0 ? 0 : x < most ? x : (int)most;
+    }
+    // f(lane of the sequence in order, parts, units up to and with it, lane of it): called for 64 sequences after the other until it returns true
+    template <typename F>
+    __device__ bool walk(const PagedArgs& a, int lane, F f) {
+        const int64_t room = (int64_t)a.cache.max_pages << a.cache.page_log;
+        most = a.most < room ? a.most : room;
+        int x = length_of(a, lane);
+        int64_t tiles = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64)                   // (64 sequences of 2^31 keys have less than 2^32 tiles)
+            tiles += (uint32_t)__builtin_amdgcn_readlane((int)lanes_upto((uint32_t)paged_tiles(b0 ? length_of(a, b0 + lane) : x)), 63);
+        PagedLength l(tiles * a.Hkv, (int64_t)a.B * a.Hkv);
+        if (a.B > 64) l.length = l.enough;
+        int before = 0;
+        for (int b0 = 0; b0 < a.B; b0 += 64) {
+            if (b0) x = length_of(a, b0 + lane);
+            const int here = a.B - b0 < 64 ? a.B - b0 : 64, t = paged_tiles(x);
+            int c, upto;
+            do {
+                c = lane < here ? 1 : 0;
+                if (__ballot(t > PAGED_WHOLE) != 0ull && lane < here) c = paged_cuts(t, l.length);
+                upto = before + (int)lanes_upto((uint32_t)(c * a.Hkv));
+            } while (!l.accepts(__builtin_amdgcn_readlane(upto, 63)));
+            int lane_in = lane;
+            const int each = c ? (t + c - 1) / c : -1;
+            if (l.sorts && a.B <= 64 && __ballot(lane < here && each != __builtin_amdgcn_readfirstlane(each)) != 0ull) {
+                int rank = lane < here ? 0 : lane;             // how many come before this lane's
+                for (int i = 0; i < here; ++i) {
+                    const int o = __builtin_amdgcn_readlane(each, i);
+                    rank += lane < here && (o > each || (o == each && i < lane)) ? 1 : 0;
+                }
+                c = __builtin_amdgcn_ds_permute(4 * rank, c);
+                lane_in = __builtin_amdgcn_ds_permute(4 * rank, lane);
+                upto = before + (int)lanes_upto((uint32_t)(c * a.Hkv));
+            }
+            if (f(b0, x, c, lane_in, upto)) return true;
+            before = __builtin_amdgcn_readlane(upto, 63);
+        }
+        return false;
+    }
+    __device__ bool find(const PagedArgs& a, int unit, int lane) {
+        auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+        return walk(a, lane, [&](int b0, int x, int c, int l, int upto) {
+            const uint64_t in = __ballot(unit < upto);
+            if (in == 0ull) return false;
+            const int at = __builtin_ctzll(in);
+            const int seq = __builtin_amdgcn_readlane(l, at);
+            cuts = u(__builtin_amdgcn_readlane(c, at));
+            b = u(b0 + seq);
+            n = u(__builtin_amdgcn_readlane(x, seq));
+            const int i = unit - (__builtin_amdgcn_readlane(upto, at) - cuts * a.Hkv);
+            kvh = u(i / cuts);
+            cut = u(i - kvh * cuts);
+            base = unit - cut;
+            return true;
+        });
+    }
+    __device__ bool find_head(const PagedArgs& a, int seq, int head, int lane) {       // the parts of one KV head
+        return walk(a, lane, [&](int b0, int x, int c, int l, int upto) {
+            const uint64_t in = __ballot(b0 + l == seq);
+            if (in == 0ull || seq < b0 || seq >= b0 + 64) return false;
+            const int at = __builtin_ctzll(in);
+            cuts = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(c, at));
+            b = seq; kvh = head; cut = 0;
+            base = __builtin_amdgcn_readfirstlane(__builtin_amdgcn_readlane(upto, at) - cuts * a.Hkv + head * cuts);
+            return true;
+        });
+    }
+};
+
 template <int D, int NH, bool E4M3>
-__global__ __launch_bounds__(PG_THREADS) void paged_kernel(PagedArgs a) {
+__global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(PagedArgs a) {
     using C = PagedCfg<D, E4M3>;
     using T = bf16_t;
     constexpr int PS = C::PS;
@@ -57,45 +142,14 @@ __global__ __launch_bounds__(PG_THREADS) void paged_kernel(PagedArgs a) {
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int m16 = lane & 15, q = lane >> 4;
     const int G = a.G, page_log = a.cache.page_log;
-    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
 
     // ---- which part of which head this workgroup has
-    const int64_t room = (int64_t)a.cache.max_pages << page_log, most = a.most < room ? a.most : room;
-    auto length_of = [&](int b) -> int {                       // of sequence b, as far as it can be
-        const int n = b < a.B ? a.len[b] : 0;
-        return n < 0 ? 0 : n < most ? n : (int)most;
-    };
-    auto tiles_of = [](int n) { return (int)(((uint32_t)n + PAGED_TILE - 1) / PAGED_TILE); };
-    int n_lane = length_of(lane);                              // of the 64 sequences at hand
-    int64_t tiles = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        if (b0) n_lane = length_of(b0 + lane);
-        const uint32_t s = lanes_upto((uint32_t)tiles_of(n_lane));                // (64 sequences of 2^31 keys are 2^32 tiles: counted one bit short of that)
-        tiles += (uint32_t)__builtin_amdgcn_readlane((int)s, 63);
-    }
-    const int length = paged_length(tiles, a.Hkv);
-    int b = -1, kvh = 0, cut = 0, cuts = 0, n = 0, before = 0;
-    for (int b0 = 0; b0 < a.B && b < 0; b0 += 64) {
-        if (a.B > 64) n_lane = length_of(b0 + lane);
-        const int mine = b0 + lane < a.B ? paged_cuts(tiles_of(n_lane), length) * a.Hkv : 0;
-        const int upto = before + (int)lanes_upto((uint32_t)mine);
-        const uint64_t in = __ballot((int)blockIdx.x < upto);
-        if (in != 0ull) {
-            const int l = __builtin_ctzll(in);
-            b = b0 + l;
-            n = __builtin_amdgcn_readlane(n_lane, l);
-            const int units = __builtin_amdgcn_readlane(mine, l), at = (int)blockIdx.x - (__builtin_amdgcn_readlane(upto, l) - units);
-            cuts = units / a.Hkv;
-            kvh = uniform(at / cuts);
-            cut = at - kvh * cuts;
-        }
-        before = __builtin_amdgcn_readlane(upto, 63);
-    }
-    if (b < 0) return;                                         // (all waves of the workgroup alike)
-    cuts = uniform(cuts); cut = uniform(cut); n = uniform(n);
+    PagedUnits w;
+    if (!w.find(a, (int)blockIdx.x, lane)) return;             // (all waves of the workgroup alike)
+    const int b = w.b, kvh = w.kvh, cut = w.cut, cuts = w.cuts, n = w.n;
     const int bk = b * a.Hkv + kvh;
-    if (cut == 0 && kvh == 0 && tid == 0 && a.len[b] > most) atomicOr(a.status, STAT_PAGE_RANGE);
-    const int all = tiles_of(n), each = (all + cuts - 1) / cuts;
+    if (cut == 0 && kvh == 0 && tid == 0 && a.len[b] > w.most) atomicOr(a.status, STAT_PAGE_RANGE);
+    const int all = paged_tiles(n), each = (all + cuts - 1) / cuts;
     const int tile0 = cut * each, tend = tile0 + each < all ? tile0 + each : all;
 
     unsigned char* stage = pg_lds + wv * C::V_BYTES;
@@ -170,8 +224,8 @@ __global__ __launch_bounds__(PG_THREADS) void paged_kernel(PagedArgs a) {
     // transpose reads.  16 bit: in a block of 16 lanes lane s points at key 4 q + s / 4 (+ 16) and value 4 (s % 4) of block i, and receives four keys of
     // column d = 16 i + s.  8 bit: lane s points at key 16 (s / 8) + 4 q + s / 2 % 4 and value 8 (s % 2), and receives the eight keys.
     const int vrow = E4M3 ? 16 * (m16 >> 3) + 4 * q + ((m16 >> 1) & 3) : 4 * q + (m16 >> 2);
-    const int vbase = vrow * C::RB + 8 * (m16 & 1);
-    const int vslot = E4M3 ? 0 : (m16 >> 1) & 1;               // 16-byte slot inside block i's bytes
+    // of block 0; block i's differs in the bits of its slot (kept as one value: the addresses of all blocks would be eight registers)
+    int vat = vrow * C::RB + 16 * (C::vswz(vrow) + (E4M3 ? 0 : (m16 >> 1) & 1)) + 8 * (m16 & 1);
 
     for (; t < tend; t += PG_WAVES) {
         wait_transfers();                                              // this tile's rows are here (the same wave reads them)
@@ -182,27 +236,23 @@ __global__ __launch_bounds__(PG_THREADS) void paged_kernel(PagedArgs a) {
             for (int i = 0; i < C::NIV; ++i)
                 if (C::RPI * i + trow >= left || !hf[C::RPI * i / 16].on) *reinterpret_cast<f32x4*>(stage + i * 1024 + 16 * lane) = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        bf16x8 kf[2][C::KC];
+        f32x4 s[NH][2];
+#pragma unroll
+        for (int h = 0; h < NH; ++h) s[h][0] = s[h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int c = 0; c < C::KC; ++c) {
+                bf16x8 kf;
                 if constexpr (E4M3) {
                     const uint4 w = __builtin_bit_cast(uint4, kr[e][c / 2]);
-                    kf[e][c] = c % 2 ? bf16_of(w.z, w.w, power_of_byte(kx[e], 0)) : bf16_of(w.x, w.y, power_of_byte(kx[e], 0));
+                    kf = c % 2 ? bf16_of(w.z, w.w, power_of_byte(kx[e], 0)) : bf16_of(w.x, w.y, power_of_byte(kx[e], 0));
                 } else {
-                    kf[e][c] = __builtin_bit_cast(bf16x8, kr[e][c]);
+                    kf = __builtin_bit_cast(bf16x8, kr[e][c]);
                 }
-            }
-        f32x4 s[NH][2];
 #pragma unroll
-        for (int h = 0; h < NH; ++h)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                s[h][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < C::KC; ++c)                        // s[h][e][r] = <k_{16 e + 4 q + r}, q_{head 16 h + m16}>
-                    s[h][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[e][c], qf[h][c], s[h][e], 0, 0, 0);
+                for (int h = 0; h < NH; ++h)                           // s[h][e][r] = <k_{16 e + 4 q + r}, q_{head 16 h + m16}>
+                    s[h][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[h][c], s[h][e], 0, 0, 0);
             }
         float vp[8];                                                   // the powers of V's rows
         if constexpr (E4M3) {
@@ -248,15 +298,16 @@ __global__ __launch_bounds__(PG_THREADS) void paged_kernel(PagedArgs a) {
             pack_frag(f, x);                                           // contraction index 8 q + r <-> key 16 (r / 4) + 4 q + r % 4
             pf[h] = f.v;
         }
+        asm volatile("" : "+v"(vat));
 #pragma unroll
         for (int i = 0; i < C::DB; ++i) {
             Frag<T> vf;
+            const unsigned char* va = stage + (vat ^ (E4M3 ? 16 : 32) * i);
             if constexpr (E4M3) {
-                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(stage + vbase + 16 * (i ^ C::vswz(vrow))));
+                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32((i32x2 __attribute__((address_space(3)))*)(va));
                 vf.v = bf16_of((uint32_t)w.x, (uint32_t)w.y, 1.0f);
             } else {
-                const unsigned char* va = stage + vbase + 16 * ((2 * i + vslot) ^ C::vswz(vrow));      // vswz(vrow + 16) is the same
-                load_frag_tr(vf, va, va + 16 * C::RB);
+                load_frag_tr(vf, va, va + 16 * C::RB);                 // vswz(vrow + 16) is the same
             }
 #pragma unroll
             for (int h = 0; h < NH; ++h) oacc[h][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf.v, pf[h], oacc[h][i], 0, 0, 0);
@@ -290,7 +341,7 @@ __global__ __launch_bounds__(PG_THREADS) void paged_kernel(PagedArgs a) {
         *reinterpret_cast<uint32_t*>(out + head * D + dd) = (uint32_t)f2bf(l > 0.f ? o0 / l : 0.f) | ((uint32_t)f2bf(l > 0.f ? o1 / l : 0.f) << 16);
         if (lse && dd == 0) lse[head] = l > 0.f ? (m * sc2 + log2f(l)) * 0.69314718055994531f : -INFINITY;
     };
-    float* shared_part = a.part + (int64_t)(blockIdx.x - cut) * G * PS;           // [part][head][PS]
+    float* shared_part = a.part + (int64_t)w.base * G * PS;           // [part][head][PS]
     const int items = G * (D / 2);                                     // two neighbouring elements of a head
     for (int idx = tid; idx < items; idx += PG_THREADS) {
         const int hd = idx / (D / 2), dd = 2 * (idx % (D / 2));
@@ -311,9 +362,15 @@ __global__ __launch_bounds__(PG_THREADS) void paged_kernel(PagedArgs a) {
         }
         if (cuts == 1) { finish(hd, dd, m, o0, o1, l); continue; }
         float* dst = shared_part + ((int64_t)cut * G + hd) * PS;
+        if (!a.done) {                                                 // paged_join_kernel's
+            *reinterpret_cast<float2*>(dst + dd) = make_float2(o0, o1);
+            if (dd == 0) *reinterpret_cast<float2*>(dst + D) = make_float2(m, l);
+            continue;
+        }
         put_shared2(dst + dd, o0, o1);
         if (dd == 0) put_shared2(dst + D, m, l);
     }
+    if (!a.done) return;
     if (blockIdx.x == 0)                                               // whatever an earlier call has left there
         for (int h = tid; h < a.clear_heads; h += PG_THREADS) clear_shared(a.done_clear + h);
     if (cuts == 1) return;
@@ -374,30 +431,83 @@ __global__ __launch_bounds__(PG_THREADS) void paged_kernel(PagedArgs a) {
     }
 }
 
-// A head's tiles are at most all there are: t / paged_length(t * Hkv ..) <= PAGED_WORKERS / Hkv, whatever t is.
-int paged_most_cuts(int Hkv, int64_t most) {
-    const int64_t tiles = (most + PAGED_TILE - 1) / PAGED_TILE, by_work = (PAGED_WORKERS + Hkv - 1) / Hkv, by_tiles = paged_cuts((int)tiles, 4);
+// Parts of heads put together by a launch of its own: grid (B * Hq), a lane for two neighbouring values of a query head and every fourth part.
+template <int D>
+__global__ __launch_bounds__(2 * D) void paged_join_kernel(PagedArgs a) {
+    constexpr int PS = D + 4, LANES = D / 2, SUBS = 4;
+    __shared__ float2 red[SUBS][LANES + 1];                    // of each subset: values, and behind them its normaliser
+    __shared__ float top[SUBS];
+    const int tid = threadIdx.x, sub = tid / LANES, dd = 2 * (tid % LANES);
+    const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, kvh = hq / a.G;
+    PagedUnits w;
+    if (!w.find_head(a, b, kvh, tid & 63) || w.cuts == 1) return;
+    const float* src = a.part + ((int64_t)w.base * a.G + hq % a.G) * PS;
+    const int64_t step = (int64_t)a.G * PS;
+    float m = -INFINITY, o0 = 0.f, o1 = 0.f, l = 0.f;
+    for (int s0 = sub; s0 < w.cuts; s0 += SUBS * PG_BATCH) {
+        float2 x[PG_BATCH], ml[PG_BATCH];
+#pragma unroll
+        for (int e = 0; e < PG_BATCH; ++e) {
+            const int s = s0 + e * SUBS < w.cuts ? s0 + e * SUBS : s0;
+            x[e] = *reinterpret_cast<const float2*>(src + s * step + dd);
+            ml[e] = *reinterpret_cast<const float2*>(src + s * step + D);
+        }
+        float m_new = m;
+#pragma unroll
+        for (int e = 0; e < PG_BATCH; ++e) m_new = fmaxf(m_new, ml[e].x);
+        const float corr = m > -INFINITY ? fast_exp2((m - m_new) * a.scale_log2e) : 0.f;
+        m = m_new; o0 *= corr; o1 *= corr; l *= corr;
+#pragma unroll
+        for (int e = 0; e < PG_BATCH; ++e) {
+            const float wgt = s0 + e * SUBS < w.cuts && ml[e].x > -INFINITY ? fast_exp2((ml[e].x - m) * a.scale_log2e) : 0.f;
+            o0 += x[e].x * wgt; o1 += x[e].y * wgt; l += ml[e].y * wgt;
+        }
+    }
+    red[sub][tid % LANES] = make_float2(o0, o1);
+    if (dd == 0) { red[sub][LANES] = make_float2(l, 0.f); top[sub] = m; }
+    __syncthreads();
+    if (sub > 0) return;
+    for (int u = 1; u < SUBS; ++u) m = fmaxf(m, top[u]);
+    o0 = o1 = l = 0.f;
+    for (int u = 0; u < SUBS; ++u) {
+        const float wgt = top[u] > -INFINITY ? fast_exp2((top[u] - m) * a.scale_log2e) : 0.f;
+        const float2 x = red[u][tid % LANES];
+        o0 += x.x * wgt; o1 += x.y * wgt; l += red[u][LANES].x * wgt;
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    reinterpret_cast<uint32_t*>(reinterpret_cast<bf16_t*>(a.out) + (int64_t)blockIdx.x * D)[dd / 2] = (uint32_t)f2bf(o0 * inv) | ((uint32_t)f2bf(o1 * inv) << 16);
+    if (a.lse && dd == 0) a.lse[blockIdx.x] = l > 0.f ? (m * a.scale_log2e + log2f(l)) * 0.69314718055994531f : -INFINITY;
+}
+
+// A head's tiles are at most all there are, and a part no shorter than these by the slots: t / paged_length(..) <= slots / Hkv, whatever t is.
+int paged_most_cuts(int B, int Hkv, int64_t most) {
+    const int64_t heads = (int64_t)B * Hkv, tiles = (most + PAGED_TILE - 1) / PAGED_TILE, by_work = (paged_slots(heads) + Hkv - 1) / Hkv;
+    const int64_t by_tiles = paged_cuts((int)tiles, paged_at_once(heads) ? PAGED_SHORTEST : PAGED_SHORTEST_MANY);
     return (int)(by_work < by_tiles ? by_work : by_tiles);
 }
 int paged_units(int B, int Hkv, int64_t most) {
-    // heads x cuts: at most one each beside the PAGED_WORKERS that the whole is cut into, and no more than all of the longest would be
-    const int64_t heads = (int64_t)B * Hkv, full = heads * paged_most_cuts(Hkv, most);
-    return (int)(full < heads + PAGED_WORKERS ? full : heads + PAGED_WORKERS);
+    // no more than the slots, or beside those the head that each part begins; and no more than all heads of the longest would be
+    const int64_t heads = (int64_t)B * Hkv, full = heads * paged_most_cuts(B, Hkv, most), slots = paged_slots(heads) + (paged_at_once(heads) ? 0 : heads);
+    return (int)(full < slots ? full : slots);
 }
 
+bool paged_joins(int B, int Hkv, int G, int64_t most) { return paged_most_cuts(B, Hkv, most) * G <= PAGED_JOIN; }
+
 template <int D, int NH, bool E4M3>
-static size_t paged_smem_t(int G, int cuts) {
+static size_t paged_smem_t(int G, int cuts, bool joins) {
     using C = PagedCfg<D, E4M3>;
     const size_t stages = (size_t)PG_WAVES * C::V_BYTES;
     const size_t merge = (size_t)PG_WAVES * G * C::PS * 4;
-    const size_t parts = cuts == 1 ? 0 : 2 * (size_t)G * cuts * 4 + 4 * (size_t)PG_THREADS * 4;
+    const size_t parts = cuts == 1 || !joins ? 0 : 2 * (size_t)G * cuts * 4 + 4 * (size_t)PG_THREADS * 4;
     const size_t m = stages > merge ? stages : merge;
     return m > parts ? m : parts;
 }
 template <int D, int NH, bool E4M3>
 static hipError_t run_paged_t(const PagedArgs& a, int units, hipStream_t st) {
-    const size_t smem = paged_smem_t<D, NH, E4M3>(a.G, paged_most_cuts(a.Hkv, a.most));
+    size_t smem = paged_smem_t<D, NH, E4M3>(a.G, paged_most_cuts(a.B, a.Hkv, a.most), a.done != nullptr);
+    if (a.B * a.Hkv <= PAGED_ALONE && smem <= 80 * 1024) smem = 80 * 1024 + 256;     // (a workgroup a compute unit, and none with two while another has none)
     hipLaunchKernelGGL((paged_kernel<D, NH, E4M3>), dim3(units), dim3(PG_THREADS), smem, st, a);
+    if (!a.done) hipLaunchKernelGGL((paged_join_kernel<D>), dim3(a.B * a.Hq), dim3(2 * D), 0, st, a);
     return hipGetLastError();
 }
 template <int D, bool E4M3>

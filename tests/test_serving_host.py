@@ -167,7 +167,7 @@ def test_cuts_of_paged_work(lib):
     rng = random.Random(3)
     for _ in range(400):
         Hkv, B = rng.choice([1, 2, 3, 8, 24, 300]), rng.choice([1, 2, 7, 64, 130])
-        most = rng.choice([1, 576, 577, 4096, 4128, rng.randint(1, 200000)])
+        most = rng.choice([1, 512, 513, 4096, 4128, rng.randint(1, 200000)])
         lens = [rng.choice([0, 1, most, rng.randint(0, most)]) for _ in range(B)]
         s = binding.make_shape(B, Hkv, Hkv, 64, most, 1, 1, "bf16")
         a, cuts, room = (C.c_int32 * B)(*lens), (C.c_int32 * B)(), C.c_int32()
