@@ -85,12 +85,12 @@ int ls_debug_page_of(const int32_t* table, int32_t max_pages, int64_t pages, int
 
 /*
  * How ls_packed_prefill counts work, of one sequence: out[0] its row blocks, [1] the 32-key steps of block j, [2] how many blocks take more than x steps, [3] the
- * bound of all blocks' steps.  And of a call: units[0] the workgroups that it cuts its items for with the workspace that ls_packed_workspace_bytes states (0: it does not),
- * [1] the items it reckons with; length: steps of a part, for so much work and so many items.
+ * bound of all blocks' steps.  And of a call: units[0] the parts that it has room for with the workspace that ls_packed_workspace_bytes states (0: it cuts no items),
+ * [1] the items it reckons with; length: steps of a part, for so much work, so many items of a KV head and the longest of them (2^28: whole).
  */
 int ls_debug_packed_counts(int32_t keys, int32_t queries, int32_t G, int32_t j, int32_t x, int64_t out[4]);
 int ls_debug_packed_units(const ls_shape* shape, int32_t packed, int64_t units[2]);
-int ls_debug_packed_length(int64_t work, int64_t items, int32_t units);
+int ls_debug_packed_length(const ls_shape* shape, double work, int32_t items, int32_t longest);
 
 /*
  * How ls_paged_attend cuts a batch of these lengths (host memory): cuts[b] of each KV head of sequence b; returns the workgroups it launches for

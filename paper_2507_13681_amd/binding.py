@@ -1,6 +1,6 @@
 """Thin binding of libloopserve (see include/loopserve.h, include/loopserve_test_hooks.h).
 
-Argument marshalling only (natively, by csrc/ls_py.c, for the calls of a serving loop; through ctypes for
+Argument marshalling only (natively, by csrc/ls_py.c and csrc/ls_pages.cpp, for the calls of a serving loop; through ctypes for
 the rest): every step of the path runs in the HIP kernels of the library.  PyTorch supplies device memory and
 the current stream.  The library must have been built
 (`python -m paper_2507_13681_amd.build` or `__graft_entry__.build()`); loading fails loudly
@@ -112,7 +112,7 @@ def load_library():
     lib.ls_debug_packed_units.restype = C.c_int
     lib.ls_debug_packed_units.argtypes = [sp, i32, C.POINTER(i64)]
     lib.ls_debug_packed_length.restype = C.c_int
-    lib.ls_debug_packed_length.argtypes = [i64, i64, i32]
+    lib.ls_debug_packed_length.argtypes = [sp, C.c_double, i32, i32]
     lib.ls_debug_paged_cuts.restype = C.c_int
     lib.ls_debug_paged_cuts.argtypes = [sp, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
     lib.ls_debug_copy_compress_score.restype = C.c_int
@@ -142,12 +142,12 @@ def load_library():
 
 
 def _load_native():
-    """The CPython module over the C ABI, built beside the library."""
+    """The CPython modules over the C ABI, built beside the library."""
     try:
-        from . import _lsnative
+        from . import _lsnative, _lspages
     except ImportError as e:
-        raise LoopServeError(f"_lsnative.so cannot be loaded ({e}): build it with `python -m paper_2507_13681_amd.build`") from e
-    return _lsnative
+        raise LoopServeError(f"_lsnative.so or _lspages.so cannot be loaded ({e}): build them with `python -m paper_2507_13681_amd.build`") from e
+    return _lsnative, _lspages
 
 
 def make_shape(B, Hq, Hkv, d, n, n_hat, w, dtype, scale=0.0) -> LsShape:
@@ -211,7 +211,7 @@ class Context:
 
     def __init__(self, shape: LsShape | None = None, budget: int = 0, device: int = 0, workspace: int | None = None):
         self.lib = load_library()
-        self.native = _load_native()
+        self.native, self.pages = _load_native()
         if workspace is None:
             workspace = workspace_bytes(shape, budget)
             if workspace == 0:
@@ -286,9 +286,9 @@ class Context:
             self._check(rc)
 
     # -- pages and packed sequences.  Rows are [rows, heads, d] where starts say whose they are, [B, heads, rows, d] otherwise, of any strides but
-    # the last; the native marshalling checks types, sizes and devices, since the library sees addresses only
+    # the last; the native marshalling checks types, sizes and devices, since the library sees addresses only (ValueError)
     def ls_packed_prefill(self, shape, q, k, v, q_starts, k_starts, out, lse=None):
-        rc = self.native.packed_prefill(self.hv, self.device, shape, q, k, v, q_starts, k_starts, out, lse)
+        rc = self.pages.packed_prefill(self.hv, self.device, shape, q, k, v, q_starts, k_starts, out, lse)
         if rc:
             self._check(rc)
 
@@ -298,18 +298,18 @@ class Context:
         return cache.struct
 
     def ls_cache_write(self, shape, cache, k, v, table, pos=None, starts=None, count=None):
-        rc = self.native.cache_write(self.hv, self.device, shape, self._pages(cache), k, v, table, pos, starts, count)
+        rc = self.pages.cache_write(self.hv, self.device, shape, self._pages(cache), k, v, table, pos, starts, count)
         if rc:
             self._check(rc)
 
     def ls_cache_read(self, shape, cache, table, k, v, pos=None, starts=None, count=None):
         """k, v: where the rows go."""
-        rc = self.native.cache_read(self.hv, self.device, shape, self._pages(cache), k, v, table, pos, starts, count)
+        rc = self.pages.cache_read(self.hv, self.device, shape, self._pages(cache), k, v, table, pos, starts, count)
         if rc:
             self._check(rc)
 
     def ls_paged_attend(self, shape, cache, q, table, lens, out, lse=None):
-        rc = self.native.paged_attend(self.hv, self.device, shape, self._pages(cache), q, table, lens, out, lse)
+        rc = self.pages.paged_attend(self.hv, self.device, shape, self._pages(cache), q, table, lens, out, lse)
         if rc:
             self._check(rc)
 

@@ -760,12 +760,8 @@ Wrong check_packed(const ls_shape* s, const ls_rows* q, const ls_rows* k, const 
     return FINE;
 }
 // Items are cut into as many parts as there is room for their results.
-int packed_units(const ls_shape* s, bool packed, size_t room) {
-    const int G = s->Hq / s->Hkv;
-    const int64_t items = ls::packed_items(s->B, s->n_hat, s->Hkv, G, packed);
-    const int64_t slots = (int64_t)(room / (ls::prefill_slot_bytes(s->d))), most = s->B > ls::PACKED_SORTED ? 0 : ls::packed_units(items, s->dtype, s->d);
-    const int64_t units = (slots < most ? slots : most) / 8 * 8;
-    return units > items ? (int)units : 0;
+ls::PackedCut packed_cut(const ls_shape* s, bool packed, size_t room) {
+    return ls::packed_cut(s->B, packed, s->n, s->n_hat, s->Hkv, s->Hq / s->Hkv, s->dtype, s->d, (int64_t)(room / ls::prefill_slot_bytes(s->d)));
 }
 size_t paged_bytes(const ls_shape* s) {
     if (ls::paged_most_cuts(s->B, s->Hkv, s->n) == 1) return 0;
@@ -786,7 +782,7 @@ int ls_cache_read(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const ls_
 size_t ls_packed_workspace_bytes(const ls_shape* s) {
     if (check_packed_shape(s).code) return 0;
     const size_t room = (size_t)1 << 40;                   // (with starts there may be more items, and so no need of parts)
-    const int units = std::max(packed_units(s, true, room), packed_units(s, false, room));
+    const int units = std::max(packed_cut(s, true, room).units, packed_cut(s, false, room).units);
     return up((size_t)units * ls::prefill_slot_bytes(s->d)) + ALIGN;
 }
 
@@ -798,9 +794,9 @@ int ls_packed_prefill(ls_ctx* c, const ls_shape* s, const ls_rows* q, const ls_r
     a.q = row_args(q); a.k = row_args(k); a.v = row_args(v); a.out = row_args(out); a.lse = lse; a.q_starts = q_starts; a.k_starts = k_starts;
     a.B = s->B; a.Hq = s->Hq; a.Hkv = s->Hkv; a.G = s->Hq / s->Hkv; a.n = (int)s->n; a.n_hat = (int)s->n_hat;
     a.scale_log2e = scale_log2e(s); a.status = c->status;
-    a.units = packed_units(s, q_starts != nullptr, c->ws_bytes);
+    a.cut = packed_cut(s, q_starts != nullptr, c->ws_bytes);
     a.part_o = reinterpret_cast<float*>(c->ws);
-    a.part_ml = a.part_o + (size_t)a.units * ls::PACKED_ROWS * s->d;
+    a.part_ml = a.part_o + (size_t)a.cut.units * ls::PACKED_ROWS * s->d;
     const OnDevice on(c->device);
     if (!on.ok) return fail(c, LS_EHIP, "ls_packed_prefill: hipSetDevice failed");
     const hipError_t e = ls::run_packed(a, s->dtype, s->d, static_cast<hipStream_t>(stream));
@@ -1011,16 +1007,19 @@ int ls_debug_page_of(const int32_t* table, int32_t max_pages, int64_t pages, int
 }
 int ls_debug_packed_counts(int32_t keys, int32_t queries, int32_t G, int32_t j, int32_t x, int64_t out[4]) {
     const ls::PackedSeq s{keys, queries};
-    out[0] = ls::packed_blocks(queries, G); out[1] = ls::packed_steps(s, G, j); out[2] = ls::packed_longer(s, G, x); out[3] = ls::packed_work(s, G);
+    out[0] = ls::packed_blocks(queries, G); out[1] = ls::packed_steps(s, G, j); out[2] = ls::packed_longer(s, G, x); out[3] = (int64_t)ls::packed_work(s, G);
     return LS_OK;
 }
 int ls_debug_packed_units(const ls_shape* s, int32_t packed, int64_t units[2]) {
     if (const Wrong w = check_packed_shape(s); w.code) return w.code;
-    units[0] = packed_units(s, packed != 0, ls_packed_workspace_bytes(s));
+    units[0] = packed_cut(s, packed != 0, ls_packed_workspace_bytes(s)).units;
     units[1] = ls::packed_items(s->B, s->n_hat, s->Hkv, s->Hq / s->Hkv, packed != 0);
     return LS_OK;
 }
-int ls_debug_packed_length(int64_t work, int64_t items, int32_t units) { return ls::packed_length(work, items, units); }
+int ls_debug_packed_length(const ls_shape* s, double work, int32_t items, int32_t longest) {
+    const ls::PackedCut c = packed_cut(s, true, ls_packed_workspace_bytes(s));
+    return c.units ? ls::packed_length(c, s->Hkv, (float)work, items, longest) : 0;
+}
 int ls_debug_paged_cuts(const ls_shape* s, const int32_t* len, int32_t* cuts, int32_t* most) {
     if (const Wrong w = check_paged_shape(s); w.code) return w.code;
     int64_t tiles = 0;

@@ -274,16 +274,33 @@ __host__ __device__ inline int packed_longer(const PackedSeq& s, int G, int x) {
     if (y >= s.queries) return 0;
     return y <= 0 ? blocks : blocks - (int)(y * G / PACKED_ROWS);
 }
-// no less than the steps of all its blocks together
-__host__ __device__ inline int64_t packed_work(const PackedSeq& s, int G) {
-    const int64_t blocks = packed_blocks(s.queries, G), before = s.keys > s.queries ? s.keys - s.queries : 0;
-    return blocks * (before / PACKED_KEYS + 4) + PACKED_ROWS / PACKED_KEYS * (blocks * (blocks + 1) / 2) / G;
+// no less than the steps of all its blocks together (each less than 4 above what is linear in j)
+__host__ __device__ inline float packed_work(const PackedSeq& s, int G) {
+    const float blocks = (float)packed_blocks(s.queries, G), before = s.keys > s.queries ? (float)((s.keys - s.queries) / PACKED_KEYS) : 0.f;
+    return blocks * (before + 4.f) + 0.5f * PACKED_ROWS / PACKED_KEYS * blocks * (blocks + 1.f) / (float)G;
 }
 constexpr int PACKED_SORTED = 64;            // with more sequences items go by sequence, whole
-constexpr int PACKED_SHORTEST = 8;           // steps of a part, at least
-__host__ __device__ inline int packed_length(int64_t work, int64_t items, int units) {           // work, items: of all KV heads; units > items
-    const int64_t each = (work + (units - items) - 1) / (units - items);
-    return each < PACKED_SHORTEST ? PACKED_SHORTEST : each < 1 << 30 ? (int)each : 1 << 30;
+// How a call cuts its items.  Parts are no more than the workgroups that are resident, so that they run at once.
+struct PackedCut {
+    int units;                // parts that there is room for; 0: items are whole
+    int least, some;          // steps of a part at least; up to this many, as many as leave a part to a compute unit
+    float step;               // what a step takes where a workgroup has its compute unit for itself, us
+};
+// What `steps` steps of `groups` workgroups take, us: where compute units have more than one, each takes longer.
+__host__ __device__ inline float packed_time(const PackedCut& c, float steps, float groups) {
+    return c.step * steps * (groups > 256.f ? 0.67f + 0.33f / 256.f * groups : 1.f);
+}
+// Steps of a part, of so much work, so many items and the longest of them (all of one of the Hkv KV heads); items and parts are no more than units / Hkv then.  Where whole items
+// take no longer than parts and what it takes to put them together (7 us, and 3 for a hundred parts), they stay whole.
+__host__ __device__ inline int packed_length(const PackedCut& c, int Hkv, float work, int items, int longest) {
+    const float each = work / (float)(c.units / Hkv - items) * 1.00001f, even = work * (float)Hkv / 256.f;
+    float l = even < (float)c.some ? even : (float)c.some;
+    l = l > (float)c.least ? l : (float)c.least;
+    l = l > each ? l : each;
+    if (!(l < (float)longest)) return 1 << 28;
+    const float parts = (float)Hkv * ((float)items + work / l);
+    if (packed_time(c, (float)longest, (float)items * (float)Hkv) < packed_time(c, l, parts) + 7.f + 0.03f * parts) return 1 << 28;
+    return (int)l + ((float)(int)l < l ? 1 : 0);
 }
 struct PackedArgs {
     RowArgs q, k, v, out;
@@ -292,7 +309,8 @@ struct PackedArgs {
     int B, Hq, Hkv, G;
     int n, n_hat;
     float scale_log2e;
-    int units;                // workgroups, if items are cut (else 0)
+    PackedCut cut;
+    bool sorted;              // more items than workgroups are resident: the longest first
     float *part_o, *part_ml;  // [units][128][d] accumulators in lane order, [units][128][2] reference and normaliser
     int32_t* status;
 };
@@ -323,7 +341,7 @@ hipError_t init_paged_kernels();
 
 hipError_t init_packed_kernels();
 hipError_t run_packed(const PackedArgs& a, int dtype, int d, hipStream_t st);
-int packed_units(int64_t items, int dtype, int d);                   // workgroups that so many items are cut for (0: they are not)
+PackedCut packed_cut(int B, bool packed, int64_t keys, int64_t queries, int Hkv, int G, int dtype, int d, int64_t room);           // with room for so many parts' results
 int64_t packed_items(int B, int64_t n_hat, int Hkv, int G, bool packed);       // no fewer than there are
 hipError_t run_move(const MoveArgs& a, bool write, int dtype, int type, int d, hipStream_t st);
 hipError_t run_paged(const PagedArgs& a, int type, int d, int units, hipStream_t st);

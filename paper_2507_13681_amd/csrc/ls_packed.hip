@@ -10,6 +10,7 @@
 // taken with the reference as it stands, and where a lane's sum exceeds a limit the step's softmax is done again with its maximum as the reference.
 // Items.  Which item a workgroup has follows from the starts, which only the device knows: a wave's lanes keep a sequence each, and count how many items take more than x steps
 // (packed_longer); a search over x finds the item of a rank, so the longest go first, whatever the lengths, and no launch ahead of this one has to put them in order.
+#include <algorithm>
 #include <type_traits>
 #include "ls_device.h"
 #include "ls_internal.h"
@@ -34,7 +35,7 @@ struct PackCfg {
     static constexpr int OUT_ROW = RB + 16;               // results on their way out: LDS bytes from row to row
     static constexpr int LDS = 2 * STEP_BYTES > PACKED_ROWS * OUT_ROW ? 2 * STEP_BYTES : PACKED_ROWS * OUT_ROW;
     static constexpr int KSTEPS = D / 16, DBLK = D / 32;
-    static constexpr int RESIDENT = F32 ? 2 : D == 64 ? 4 : 3;                // workgroups of a CU
+    static constexpr int RESIDENT = F32 ? (D == 128 ? 1 : 2) : D == 64 ? 4 : 3;         // workgroups of a CU, at least (fp32 at d = 128 spills with two)
     // slot swizzles (XOR on the 16-byte slot index inside a row), so that fragment reads touch each bank once
     __device__ static constexpr int kswz(int row) { return F32 ? row & 15 : D == 128 ? (row & 3) : (((row >> 1) & 3) | (((row >> 3) & 1) << 2)); }
     __device__ static constexpr int vswz(int row) { return F32 ? row & 15 : D == 128 ? ((row & 3) << 2) : (((row >> 1) & 1) << 2); }
@@ -71,13 +72,7 @@ struct PackedWork {
     // the item of rank r among those of a KV head, the longest first; false: there are not so many.  (At most 64 sequences.)
     __device__ bool find(int r) {
         if (r >= longer(-1)) return false;
-        int lo = -1, hi = 0;                               // rank r takes more than lo steps, and at most hi
-        {
-            int most = seq.queries > 0 ? packed_steps(seq, G, packed_blocks(seq.queries, G) - 1) : 0;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) { const int y = __shfl_xor(most, o, 64); most = y > most ? y : most; }
-            hi = __builtin_amdgcn_readfirstlane(most);
-        }
+        int lo = -1, hi = longest() + 8;                   // rank r takes more than lo steps, and at most hi (a float has the longest, 2^26 at most, to within 4)
         while (hi - lo > 1) {
             const int x = (lo + hi) >> 1;
             if (longer(x) <= r) hi = x; else lo = x;
@@ -109,22 +104,48 @@ struct PackedWork {
         return false;
     }
     // steps of a part of a call that cuts its items
-    __device__ void cut_length(const PackedArgs& a) {
-        const int64_t w = packed_work(seq, G);
-        // (sums of 64-bit words, by halves of 24 bits and the rest)
-        const int64_t work = (int64_t)lanes_sum((uint32_t)(w & 0xFFFFFF)) + ((int64_t)lanes_sum((uint32_t)(w >> 24)) << 24);
-        length = packed_length(work * a.Hkv, (int64_t)longer(-1) * a.Hkv, a.units);
+    __device__ int longest() const {                       // steps of the longest item
+        const float most = seq.queries > 0 ? (float)packed_steps(seq, G, packed_blocks(seq.queries, G) - 1) : 0.f;
+        return __builtin_amdgcn_readfirstlane((int)wave_largest(most));
     }
-    // items of a KV head that have a part p, of p = p0 + lane
-    __device__ int having(int p0) const {
+    __device__ void cut_length(const PackedArgs& a) {
+        length = __builtin_amdgcn_readfirstlane(packed_length(a.cut, a.Hkv, wave_sum(packed_work(seq, G)), longer(-1), longest()));
+    }
+    __device__ int longer_than_part(const PackedSeq& x, int p) const {          // blocks that have a part p
+        const int64_t steps = (int64_t)p * length;
+        return p == 0 ? packed_longer(x, G, -1) : steps > 1 << 28 ? 0 : packed_longer(x, G, (int)steps);
+    }
+    // blocks that have a part p0 + lane, of sequences 0 .. most - 1 (with `before`: of those before sequence `stop`)
+    __device__ int having(const PackedArgs& a, int p0, int stop = 0, int* before = nullptr) const {
         int sum = 0;
-        for (int i = 0; i < 64; ++i) {
+        for (int i = 0; i < a.B; ++i) {
+            if (before && i == stop) *before = sum;
             const PackedSeq x{__builtin_amdgcn_readlane(seq.keys, i), __builtin_amdgcn_readlane(seq.queries, i)};
-            if (x.queries == 0) continue;
-            const int64_t steps = (int64_t)(p0 + lane) * length;
-            sum += p0 + lane == 0 ? packed_longer(x, G, -1) : steps > 1 << 28 ? 0 : packed_longer(x, G, (int)steps);
+            if (x.queries > 0) sum += longer_than_part(x, p0 + lane);
         }
         return sum;
+    }
+    // Units of a KV head in the order of parts, and those by sequence and block: unit r is ..  (All run at once, so that their order does not matter.)
+    __device__ bool find_part(const PackedArgs& a, int r) {
+        cut_length(a);
+        int before = 0;
+        part = -1;
+        for (int p0 = 0; part < 0; p0 += 64) {
+            const int mine = having(a, p0), upto = before + (int)lanes_upto((uint32_t)mine);
+            const uint64_t in = __ballot(r < upto);
+            if (in != 0ull) {
+                const int l = __builtin_ctzll(in);
+                part = p0 + l;
+                r -= __builtin_amdgcn_readlane(upto - mine, l);
+            } else if (__builtin_amdgcn_readlane(mine, 63) == 0) {
+                return false;
+            }
+            before = __builtin_amdgcn_readlane(upto, 63);
+        }
+        const int upto = (int)lanes_upto((uint32_t)longer_than_part(seq, part));
+        s = __builtin_ctzll(__ballot(r < upto));
+        block = packed_blocks(__builtin_amdgcn_readlane(seq.queries, s), G) - 1 - (r - (s > 0 ? __builtin_amdgcn_readlane(upto, s - 1) : 0));          // (the longest first)
+        return true;
     }
 };
 
@@ -151,32 +172,13 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
         else if (a.Hkv % 8 == 0) { kvh = x + 8 * (i % (a.Hkv / 8)); rank = i / (a.Hkv / 8); }
         else { kvh = u % a.Hkv; rank = u / a.Hkv; }
     }
-    if (a.units) {
-        w.cut_length(a);
-        int before = 0, found = -1;
-        for (int p0 = 0; found < 0; p0 += 64) {
-            const int mine = w.having(p0), upto = before + (int)lanes_upto((uint32_t)mine);
-            const uint64_t in = __ballot(rank < upto);
-            if (in != 0ull) {
-                const int l = __builtin_ctzll(in);
-                found = p0 + l;
-                rank -= __builtin_amdgcn_readlane(upto - mine, l);
-            } else if (__builtin_amdgcn_readlane(mine, 63) == 0) {
-                return;                                    // no such unit
-            }
-            before = __builtin_amdgcn_readlane(upto, 63);
-        }
-        w.part = found;
-        if (!w.find(rank)) return;
-    } else if (a.B <= PACKED_SORTED ? !w.find(rank) : !w.find_in_order(a, rank)) {
-        return;
-    }
+    if (!(a.cut.units ? w.find_part(a, rank) : a.sorted ? w.find(rank) : w.find_in_order(a, rank))) return;
     const int s = uniform(w.s), block = uniform(w.block), sl64 = s & 63;
     const int nk = __builtin_amdgcn_readlane(w.seq.keys, sl64), nq = __builtin_amdgcn_readlane(w.seq.queries, sl64);
     const int64_t q0 = a.q_starts ? a.q_starts[s] : 0, k0 = a.k_starts ? a.k_starts[s] : 0, pad = a.q_starts ? 0 : s;
     const int steps = packed_steps(PackedSeq{nk, nq}, G, block);
-    const int h0 = w.part * w.length, h1 = steps - h0 > w.length ? h0 + w.length : steps;            // steps of this part
-    const bool cut = steps > w.length;
+    const int length = uniform(w.length), h0 = uniform(w.part) * length, h1 = steps - h0 > length ? h0 + length : steps;         // steps of this part
+    const bool cut = steps > length;
     // rows
     const int64_t rows = (int64_t)nq * G, rho0 = (int64_t)PACKED_ROWS * block + 32 * wv;
     const bool rows_here = rho0 < rows;
@@ -332,6 +334,7 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
             __builtin_amdgcn_sched_barrier(0);
         }
         if (PACKED_KEYS * h + PACKED_KEYS - 1 > pos_least) {
+            asm volatile("");                              // (few steps: a branch, no selects in the others)
             const int lim = pos - PACKED_KEYS * h - 4 * g;
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = 8 * (r / 4) + r % 4 <= lim ? x[r] : -INFINITY;
@@ -411,6 +414,7 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
 
     float l_tot = l_run + xor32(l_run);
     if (cut) {
+        if (!rows_here) return;
         float* o = a.part_o + (int64_t)blockIdx.x * (PACKED_ROWS * D) + wv * (C::DBLK * 4 * 256) + lane * 4;
 #pragma unroll
         for (int i = 0; i < C::DBLK; ++i)
@@ -450,55 +454,64 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
     }
 }
 
-// The parts of items put together: grid (items of all KV heads, 4 waves' rows), a wave for each block of 32 output values.  Parts of an item lie as its rank has them: part p's units
-// follow those of the parts before it, in the order of ranks.
+// The parts of items put together: for each item 4 waves' rows x blocks of 32 output values, a workgroup for one after the other, a wave of it for every fourth part.
+constexpr int PK_JOIN_GROUPS = 1024;
 template <typename T, int D>
-__global__ __launch_bounds__(2 * D) void packed_join_kernel(PackedArgs a) {
+__global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
     using C = PackCfg<T, D>;
+    constexpr int SUBS = 4, NB = 4;                        // subsets of parts, parts in flight
+    __shared__ f32x4 red[SUBS][4][64];
+    __shared__ float2 red_ml[SUBS][32];
     const int tid = threadIdx.x, lane = tid & 63;
-    const int i = __builtin_amdgcn_readfirstlane(tid >> 6), wv = blockIdx.y;               // output block, wave whose rows these are
+    const int sub = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r32 = lane & 31, g = lane >> 5, G = a.G;
     PackedWork w;
     w.G = G; w.lane = lane; w.s = 0; w.block = 0;
     w.keep(a, 0);
     w.cut_length(a);
-    const int kvh = blockIdx.x % a.Hkv, rank = blockIdx.x / a.Hkv;
-    if (rank >= w.longer(w.length) || !w.find(rank)) return;                              // not cut
+    if (w.length == 1 << 28) return;                       // there are none
+    constexpr int PER = 4 * C::DBLK;
+    const int items = w.longer(-1) * a.Hkv;
+    for (int64_t at = blockIdx.x; at < (int64_t)items * PER; at += gridDim.x) {
+    const int item = (int)(at / PER), wv = (int)(at % PER) / C::DBLK, i = (int)(at % PER) % C::DBLK;        // item, wave whose rows these are, output block
+    const int kvh = item % a.Hkv;
+    w.find_in_order(a, item / a.Hkv);
     const int s = __builtin_amdgcn_readfirstlane(w.s), block = __builtin_amdgcn_readfirstlane(w.block);
     const int nk = __builtin_amdgcn_readlane(w.seq.keys, s), nq = __builtin_amdgcn_readlane(w.seq.queries, s);
-    const int parts = (packed_steps(PackedSeq{nk, nq}, G, block) + w.length - 1) / w.length;
     const int64_t rows = (int64_t)nq * G, rho0 = (int64_t)PACKED_ROWS * block + 32 * wv;
-    if (rho0 >= rows) return;
+    const int steps = packed_steps(PackedSeq{nk, nq}, G, block);
+    const int parts = (steps + w.length - 1) / w.length;
+    if (rho0 >= rows || parts <= 1) continue;
     f32x4 acc[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) acc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
     float M = -INFINITY, L = 0.f;
     int before = 0;                                        // units of the parts before those at hand
     for (int p0 = 0; p0 < parts; p0 += 64) {
-        const int mine = w.having(p0), upto = before + (int)lanes_upto((uint32_t)mine);
+        int ahead = 0;                                     // of the part of a lane: units of the sequences before this one
+        const int mine = w.having(a, p0, s, &ahead), upto = before + (int)lanes_upto((uint32_t)mine);
+        // this block's unit of the part of a lane (packed_kernel), and which workgroup that was
+        const int rank = upto - mine + ahead + packed_blocks(nq, G) - 1 - block;
+        int unit;
+        if (8 % a.Hkv == 0) { const int per = 8 / a.Hkv; unit = rank / per * 8 + kvh * per + rank % per; }
+        else if (a.Hkv % 8 == 0) unit = (rank * (a.Hkv / 8) + kvh / 8) * 8 + kvh % 8;
+        else unit = rank * a.Hkv + kvh;
+        unit = unit < a.cut.units ? unit : a.cut.units - 1;
         const int here = parts - p0 < 64 ? parts - p0 : 64;
-        constexpr int NB = 4;                              // parts in flight
-        for (int e0 = 0; e0 < here; e0 += NB) {
+        for (int e0 = sub; e0 < here; e0 += SUBS * NB) {
             float2 ml[NB];
             f32x4 x[NB][4];
 #pragma unroll
             for (int e = 0; e < NB; ++e) {
-                const int l = e0 + e < here ? e0 + e : here - 1;
-                const int at = __builtin_amdgcn_readlane(upto - mine, l) + rank;
-                // the unit that this rank of this KV head is (packed_kernel)
-                int unit;
-                if (8 % a.Hkv == 0) { const int per = 8 / a.Hkv; unit = at / per * 8 + kvh * per + at % per; }
-                else if (a.Hkv % 8 == 0) unit = (at * (a.Hkv / 8) + kvh / 8) * 8 + kvh % 8;
-                else unit = at * a.Hkv + kvh;
-                unit = unit < a.units ? unit : a.units - 1;
-                ml[e] = reinterpret_cast<const float2*>(a.part_ml)[(int64_t)unit * PACKED_ROWS + 32 * wv + r32];
-                const float* o = a.part_o + (int64_t)unit * (PACKED_ROWS * D) + wv * (C::DBLK * 4 * 256) + i * 4 * 256 + lane * 4;
+                const int u = __builtin_amdgcn_readlane(unit, e0 + e * SUBS < here ? e0 + e * SUBS : e0);
+                ml[e] = reinterpret_cast<const float2*>(a.part_ml)[(int64_t)u * PACKED_ROWS + 32 * wv + r32];
+                const float* o = a.part_o + (int64_t)u * (PACKED_ROWS * D) + wv * (C::DBLK * 4 * 256) + i * 4 * 256 + lane * 4;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) x[e][k] = *reinterpret_cast<const f32x4*>(o + k * 256);
             }
             float m_new = M;
 #pragma unroll
-            for (int e = 0; e < NB; ++e) if (e0 + e < here) m_new = fmaxf(m_new, ml[e].x);
+            for (int e = 0; e < NB; ++e) m_new = fmaxf(m_new, ml[e].x);
             const float corr = M > -INFINITY ? fast_exp2(M - m_new) : 0.f;
             M = m_new;
             L *= corr;
@@ -506,8 +519,7 @@ __global__ __launch_bounds__(2 * D) void packed_join_kernel(PackedArgs a) {
             for (int k = 0; k < 4; ++k) acc[k] *= corr;
 #pragma unroll
             for (int e = 0; e < NB; ++e) {
-                if (e0 + e >= here) break;
-                const float wgt = ml[e].x > -INFINITY ? fast_exp2(ml[e].x - M) : 0.f;
+                const float wgt = e0 + e * SUBS < here && ml[e].x > -INFINITY ? fast_exp2(ml[e].x - M) : 0.f;
                 L += ml[e].y * wgt;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) acc[k] += x[e][k] * wgt;
@@ -515,41 +527,68 @@ __global__ __launch_bounds__(2 * D) void packed_join_kernel(PackedArgs a) {
         }
         before = __builtin_amdgcn_readlane(upto, 63);
     }
-    if (rho0 + r32 >= rows) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) red[sub][k][lane] = acc[k];
+    if (lane < 32) red_ml[sub][lane] = make_float2(M, L);
+    __syncthreads();
+    // wave `sub` finishes values 8 sub + 4 g .. of the block
+    float top = -INFINITY;
+    float2 ml[SUBS];
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) { ml[u] = red_ml[u][r32]; top = fmaxf(top, ml[u].x); }
+    f32x4 y = f32x4{0.f, 0.f, 0.f, 0.f};
+    L = 0.f;
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) {
+        const float wgt = ml[u].x > -INFINITY ? fast_exp2(ml[u].x - top) : 0.f;
+        L += ml[u].y * wgt;
+        y += red[u][sub][lane] * wgt;
+    }
+    __syncthreads();                                       // (before the next item's)
+    if (rho0 + r32 >= rows) continue;
     const int64_t rho = rho0 + r32, qi = (uint32_t)rho / (uint32_t)G, hd = kvh * (int64_t)G + (rho - qi * G);
     const int64_t q0 = a.q_starts ? a.q_starts[s] : 0, pad = a.q_starts ? 0 : s;
-    const float inv = L > 0.f ? 1.0f / L : 0.f;
-    unsigned char* og = a.out.data + (pad * a.out.seq + (q0 + qi) * a.out.row + hd * a.out.head) * Elem<T>::bytes;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        const f32x4 y = acc[k] * inv;
-        unsigned char* dst = og + (32 * i + 8 * k + 4 * g) * Elem<T>::bytes;
-        if constexpr (C::F32) *reinterpret_cast<f32x4*>(dst) = y;
-        else *reinterpret_cast<__attribute__((ext_vector_type(4))) __bf16*>(dst) = __builtin_convertvector(y, __attribute__((ext_vector_type(4))) __bf16);
+    y *= L > 0.f ? 1.0f / L : 0.f;
+    unsigned char* dst = a.out.data + (pad * a.out.seq + (q0 + qi) * a.out.row + hd * a.out.head + 32 * i + 8 * sub + 4 * g) * Elem<T>::bytes;
+    if constexpr (C::F32) *reinterpret_cast<f32x4*>(dst) = y;
+    else *reinterpret_cast<__attribute__((ext_vector_type(4))) __bf16*>(dst) = __builtin_convertvector(y, __attribute__((ext_vector_type(4))) __bf16);
+    if (a.lse && i == 0 && sub == 0 && g == 0)
+        a.lse[(a.q_starts ? hd * a.n_hat + q0 : ((int64_t)s * a.Hq + hd) * a.n_hat) + qi] = L > 0.f ? (log2f(L) + top) * 0.69314718055994531f : -INFINITY;
     }
-    if (a.lse && i == 0 && g == 0)
-        a.lse[(a.q_starts ? hd * a.n_hat + q0 : ((int64_t)s * a.Hq + hd) * a.n_hat) + qi] = L > 0.f ? (log2f(L) + M) * 0.69314718055994531f : -INFINITY;
 }
 
 int64_t packed_items(int B, int64_t n_hat, int Hkv, int G, bool packed) {
     if (packed) return Hkv * ((n_hat * G + PACKED_ROWS - 1) / PACKED_ROWS + B);
     return (int64_t)B * Hkv * ((n_hat * G + PACKED_ROWS - 1) / PACKED_ROWS);
 }
-// Items are cut where they are fewer than workgroups are resident.
-int packed_units(int64_t items, int dtype, int d) {
-    const int resident = 256 * (dtype == 1 ? 2 : d == 64 ? 4 : 3);
-    return items < resident ? resident : 0;
+static int packed_resident(int dtype, int d) { return 256 * (dtype == 1 ? 2 : d == 64 ? 4 : 3); }
+PackedCut packed_cut(int B, bool packed, int64_t keys, int64_t queries, int Hkv, int G, int dtype, int d, int64_t room) {
+    const int64_t items = packed_items(B, queries, Hkv, G, packed);
+    const int resident = packed_resident(dtype, d);
+    PackedCut c{0, dtype == 1 ? 1 : 8, dtype == 1 ? 1 << 20 : 12, (dtype == 1 ? 4.f : 0.65f) * (d == 64 ? 0.5f : 1.f)};
+    const int64_t units = (room < resident ? room : resident) / 8 * 8;
+    if (units <= items || B > PACKED_SORTED) return c;
+    c.units = (int)units;
+    // Where the host sees that nothing will be cut, there is no launch that looks for parts, 3 us: of equal sequences what the device finds, of others the least that it may find
+    const PackedSeq s{(int)keys, (int)queries};
+    const int blocks = packed_blocks(s.queries, G), longest = packed_steps(s, G, blocks - 1);
+    const bool whole = !packed || B == 1 ? packed_length(c, Hkv, packed_work(s, G) * (float)B, blocks * B, longest) == 1 << 28
+                                         : packed_time(c, (float)((keys + PACKED_KEYS - 1) / PACKED_KEYS), (float)items) < packed_time(c, (float)c.least, 1.f) + 7.f;
+    if (whole) c.units = 0;
+    return c;
 }
 
 template <typename T, int D>
-static hipError_t run_packed_t(const PackedArgs& a, hipStream_t st) {
+static hipError_t run_packed_t(PackedArgs a, hipStream_t st) {
+    constexpr int dtype = PackCfg<T, D>::F32 ? 1 : 0;
     const int64_t items = packed_items(a.B, a.n_hat, a.Hkv, a.G, a.q_starts != nullptr);
+    a.sorted = a.B <= PACKED_SORTED && items > packed_resident(dtype, D);
     // the ranks of a KV head's items, rounded up to what the XCDs share
-    int64_t groups = a.units ? a.units : (items + 7) / 8 * 8;
-    if (!a.units && 8 % a.Hkv != 0 && a.Hkv % 8 != 0) groups = items;
+    int64_t groups = a.cut.units ? a.cut.units : (items + 7) / 8 * 8;
+    if (!a.cut.units && 8 % a.Hkv != 0 && a.Hkv % 8 != 0) groups = items;
     if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
     hipLaunchKernelGGL((packed_kernel<T, D>), dim3((uint32_t)groups), dim3(PK_THREADS), (PackCfg<T, D>::LDS), st, a);
-    if (a.units) hipLaunchKernelGGL((packed_join_kernel<T, D>), dim3((uint32_t)items, 4), dim3(2 * D), 0, st, a);
+    if (a.cut.units) hipLaunchKernelGGL((packed_join_kernel<T, D>), dim3((uint32_t)std::min<int64_t>(items * 4 * PackCfg<T, D>::DBLK, PK_JOIN_GROUPS)), dim3(256), 0, st, a);
     return hipGetLastError();
 }
 hipError_t init_packed_kernels() {

@@ -9,9 +9,7 @@
 #include "../../include/loopserve.h"
 
 static PyObject *s_data_ptr, *s_is_cuda, *s_is_contiguous, *s_size;   /* interned names */
-static PyObject *s_shape, *s_stride, *s_dtype, *s_get_device;
 static PyObject *get_device, *get_raw_stream;                         /* torch._C functions */
-static PyObject *t_bf16, *t_f32, *t_i32;                              /* torch types */
 
 /* Device address of a contiguous GPU tensor; None is NULL.  0 on success. */
 static int dev_ptr(PyObject* t, void** out) {
@@ -126,133 +124,10 @@ DEF(decode_attend) {  /* ctx, shape, q, k_c, v_c, cnt, k_t, v_t, out, lse */
     RETURN(ls_decode_attend(ctx, &sh, cap, T, q, kc, vc, cnt, kt, vt, out, lse, st));
 }
 
-/* ---- the calls on pages and packed sequences, which take tensors of any strides: everything that the library cannot see of a tensor
- * (its type, its sizes, its device) is checked here */
-static int wrong(const char* name, const char* what) { PyErr_Format(PyExc_ValueError, "%s: %s", name, what); return -1; }
-
-/* A tensor on GPU `device` of this type: its address. */
-static int typed_ptr(PyObject* t, const char* name, PyObject* type, long device, void** out) {
-    PyObject* r = PyObject_GetAttr(t, s_is_cuda);
-    if (!r) return -1;
-    const int gpu = r == Py_True;
-    Py_DECREF(r);
-    if (!gpu) return wrong(name, "must be a device tensor");
-    if (!(r = PyObject_GetAttr(t, s_dtype))) return -1;
-    const int same = r == type;
-    Py_DECREF(r);
-    if (!same) return wrong(name, "has another type than the call takes");
-    if (!(r = PyObject_CallMethodNoArgs(t, s_get_device))) return -1;
-    const long on = PyLong_AsLong(r);
-    Py_DECREF(r);
-    if (on == -1 && PyErr_Occurred()) return -1;
-    if (on != device) return wrong(name, "is not on the context's GPU");
-    if (!(r = PyObject_CallMethodNoArgs(t, s_data_ptr))) return -1;
-    *out = PyLong_AsVoidPtr(r);
-    Py_DECREF(r);
-    return *out == NULL && PyErr_Occurred() ? -1 : 0;
-}
-/* Sizes or strides of a tensor: how many, or -1. */
-static int numbers(PyObject* seq, int64_t* out, int most) {
-    if (!seq) return -1;
-    int n = -1;
-    if (PyTuple_Check(seq)) {
-        n = (int)PyTuple_GET_SIZE(seq);
-        for (int i = 0; i < n && i < most; ++i) out[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(seq, i));
-    }
-    Py_DECREF(seq);
-    return PyErr_Occurred() ? -1 : n;
-}
-/* A contiguous tensor of these sizes (-1: any); None is NULL. */
-static int plain_ptr(PyObject* t, const char* name, PyObject* type, long device, int dims, const int64_t* want, void** out) {
-    if (t == Py_None) { *out = NULL; return 0; }
-    if (typed_ptr(t, name, type, device, out)) return -1;
-    int64_t size[4];
-    int ok = numbers(PyObject_GetAttr(t, s_shape), size, 4) == dims;
-    for (int i = 0; ok && i < dims; ++i) ok = want[i] < 0 || size[i] == want[i];
-    if (!ok) return PyErr_Occurred() ? -1 : wrong(name, "has other sizes than the call takes");
-    PyObject* r = PyObject_CallMethodNoArgs(t, s_is_contiguous);
-    if (!r) return -1;
-    ok = r == Py_True;
-    Py_DECREF(r);
-    return ok ? 0 : wrong(name, "must be contiguous");
-}
-/* Rows: packed [rows,H,d], else [B,H,rows,d], of any strides but the last, which is one. */
-static int rows_of(PyObject* t, const char* name, const ls_shape* s, long device, int packed, int64_t rows, int64_t H, ls_rows* out) {
-    int64_t size[4], step[4];
-    if (typed_ptr(t, name, s->dtype == LS_BF16 ? t_bf16 : t_f32, device, &out->data)) return -1;
-    const int dims = numbers(PyObject_GetAttr(t, s_shape), size, 4);
-    if (dims < 0 || numbers(PyObject_CallMethodNoArgs(t, s_stride), step, 4) < 0) return PyErr_Occurred() ? -1 : wrong(name, "is no tensor");
-    const int64_t packed_size[3] = {rows, H, s->d}, padded_size[4] = {s->B, H, rows, s->d};
-    int ok = dims == (packed ? 3 : 4);
-    for (int i = 0; ok && i < dims; ++i) ok = size[i] == (packed ? packed_size[i] : padded_size[i]);
-    if (!ok) return wrong(name, packed ? "must be [rows, heads, d] of the shape's numbers" : "must be [B, heads, rows, d] of the shape's numbers");
-    if (step[dims - 1] != 1) return wrong(name, "the values of a row must be neighbours");
-    for (int i = 0; i < dims; ++i) if (size[i] == 1) step[i] = 0;         /* (never taken, whatever it says) */
-    if (packed) { out->seq = 0; out->row = step[0]; out->head = step[1]; }
-    else { out->seq = step[0]; out->head = step[1]; out->row = step[2]; }
-    return 0;
-}
-static int cache_of(PyObject* o, ls_cache* c) {
-    Py_buffer b;
-    if (PyObject_GetBuffer(o, &b, PyBUF_SIMPLE) != 0) return -1;
-    const int ok = b.len == (Py_ssize_t)sizeof(ls_cache);
-    if (ok) memcpy(c, b.buf, sizeof(ls_cache));
-    PyBuffer_Release(&b);
-    if (!ok) PyErr_SetString(PyExc_TypeError, "cache must be a PagedCache");
-    return ok ? 0 : -1;
-}
-/* The stream that PyTorch currently issues to on a GPU. */
-static int stream_on(PyObject* device, void** out) {
-    PyObject* r = PyObject_CallOneArg(get_raw_stream, device);
-    if (!r) return -1;
-    *out = PyLong_AsVoidPtr(r);
-    Py_DECREF(r);
-    return *out == NULL && PyErr_Occurred() ? -1 : 0;
-}
-#define DEVICE(i) const long device = PyLong_AsLong(a[i]); if (device == -1 && PyErr_Occurred()) return NULL
-#define ROWS(name, i, packed, rows, heads) ls_rows name; if (rows_of(a[i], #name, &sh, device, packed, rows, heads, &name)) return NULL
-#define PLAIN(name, i, type, dims, ...) void* name; { const int64_t want[4] = {__VA_ARGS__}; if (plain_ptr(a[i], #name, type, device, dims, want, &name)) return NULL; }
-#define STREAM_ON(i) void* st; if (stream_on(a[i], &st)) return NULL
-#define CACHE(i) ls_cache cache; if (cache_of(a[i], &cache)) return NULL
-
-DEF(packed_prefill) { /* ctx, device, shape, q, k, v, q_starts, k_starts, out, lse */
-    (void)self; ARGS(10) CTX(0); DEVICE(1); SHAPE(2);
-    const int packed = a[6] != Py_None;
-    ROWS(q, 3, packed, sh.n_hat, sh.Hq); ROWS(k, 4, packed, sh.n, sh.Hkv); ROWS(v, 5, packed, sh.n, sh.Hkv);
-    PLAIN(q_starts, 6, t_i32, 1, (int64_t)sh.B + 1) PLAIN(k_starts, 7, t_i32, 1, (int64_t)sh.B + 1)
-    ROWS(out, 8, packed, sh.n_hat, sh.Hq);
-    void* lse = NULL;
-    const int64_t packed_lse[2] = {sh.Hq, sh.n_hat}, padded_lse[3] = {sh.B, sh.Hq, sh.n_hat};
-    if (plain_ptr(a[9], "lse", t_f32, device, packed ? 2 : 3, packed ? packed_lse : padded_lse, &lse)) return NULL;
-    STREAM_ON(1);
-    RETURN(ls_packed_prefill(ctx, &sh, &q, &k, &v, q_starts, k_starts, &out, lse, st));
-}
-/* ctx, device, shape, cache, k, v, table, pos, starts, count */
-#define MOVE(call) \
-    (void)self; ARGS(10) CTX(0); DEVICE(1); SHAPE(2); CACHE(3); \
-    const int packed = a[8] != Py_None; \
-    ROWS(k, 4, packed, sh.n_hat, sh.Hkv); ROWS(v, 5, packed, sh.n_hat, sh.Hkv); \
-    PLAIN(table, 6, t_i32, 2, sh.B, -1) PLAIN(pos, 7, t_i32, 1, sh.B) PLAIN(starts, 8, t_i32, 1, (int64_t)sh.B + 1) PLAIN(count, 9, t_i32, 1, sh.B) \
-    int32_t pages = 0; \
-    if (table && dim_of(a[6], 1, &pages)) return NULL; \
-    STREAM_ON(1); \
-    RETURN(call(ctx, &sh, &cache, &k, &v, starts, count, table, pages, pos, st))
-DEF(cache_write) { MOVE(ls_cache_write); }
-DEF(cache_read) { MOVE(ls_cache_read); }
-DEF(paged_attend) {   /* ctx, device, shape, cache, q, table, len, out, lse */
-    (void)self; ARGS(9) CTX(0); DEVICE(1); SHAPE(2); CACHE(3);
-    PLAIN(q, 4, t_bf16, 3, sh.B, sh.Hq, sh.d) PLAIN(table, 5, t_i32, 2, sh.B, -1) PLAIN(lens, 6, t_i32, 1, sh.B)
-    PLAIN(out, 7, t_bf16, 3, sh.B, sh.Hq, sh.d) PLAIN(lse, 8, t_f32, 2, sh.B, sh.Hq)
-    int32_t pages = 0;
-    if (table && dim_of(a[5], 1, &pages)) return NULL;
-    STREAM_ON(1);
-    RETURN(ls_paged_attend(ctx, &sh, &cache, q, table, pages, lens, out, lse, st));
-}
-
 static PyMethodDef methods[] = {
 #define M(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, NULL}
     M(score), M(score_window), M(select_lines), M(select_exact), M(merge_lines), M(sparse_prefill), M(kv_compress),
-    M(decode_attend), M(packed_prefill), M(cache_write), M(cache_read), M(paged_attend), {NULL, NULL, 0, NULL}};
+    M(decode_attend), {NULL, NULL, 0, NULL}};
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lsnative", NULL, -1, methods, NULL, NULL, NULL, NULL};
 
 PyMODINIT_FUNC PyInit__lsnative(void) {
@@ -260,17 +135,6 @@ PyMODINIT_FUNC PyInit__lsnative(void) {
     s_is_cuda = PyUnicode_InternFromString("is_cuda");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_size = PyUnicode_InternFromString("size");
-    s_shape = PyUnicode_InternFromString("shape");
-    s_stride = PyUnicode_InternFromString("stride");
-    s_dtype = PyUnicode_InternFromString("dtype");
-    s_get_device = PyUnicode_InternFromString("get_device");
-    PyObject* torch = PyImport_ImportModule("torch");
-    if (!torch) return NULL;
-    t_bf16 = PyObject_GetAttrString(torch, "bfloat16");
-    t_f32 = PyObject_GetAttrString(torch, "float32");
-    t_i32 = PyObject_GetAttrString(torch, "int32");
-    Py_DECREF(torch);
-    if (!t_bf16 || !t_f32 || !t_i32) return NULL;
     PyObject* c = PyImport_ImportModule("torch._C");
     if (!c) return NULL;
     get_device = PyObject_GetAttrString(c, "_cuda_getDevice");

@@ -153,9 +153,9 @@ def test_parts_of_packed_items_fit_into_their_units(lib):
         assert items * Hkv <= units[1]
         if n == 0:
             continue
-        cut += 1
         assert n > units[1] and n % 8 == 0
-        length = lib.ls_debug_packed_length(work * Hkv, items * Hkv, n)
+        length = lib.ls_debug_packed_length(C.byref(s), work, items, max(steps, default=0))
+        cut += length < 1 << 28
         parts = sum(max(1, -(-x // length)) for x in steps)
         assert parts <= n // Hkv, (parts, n, Hkv)
         assert n * (128 * d + 256) * 4 <= lib.ls_packed_workspace_bytes(C.byref(s))

@@ -12,7 +12,6 @@ from tests.test_transfer_waits import _transfers_at_barriers
 TRANSFERS = {"ls_paged.hip": [("paged_kernelI", 8)], "ls_packed.hip": [("packed_kernelI", 4)], "ls_cache.hip": []}
 # bf16 instances of which a CU is to have so many waves on each of its SIMDs at once: 512 registers are shared by them
 WAVES = {"ls_packed.hip": {"packed_kernelINS_6bf16_tELi128E": 3, "packed_kernelINS_6bf16_tELi64E": 4}}
-SPILLS = {"packed_kernelIfLi128E"}                         # fp32 at d = 128: more values than registers
 
 
 @pytest.mark.parametrize("source", TRANSFERS)
@@ -44,8 +43,7 @@ def test_built_kernels(tmp_path, source):
     field = lambda k, name: int(re.search(rf"^\s*\.{name}:\s+(\d+)", k, flags=re.M)[1])
     assert told
     for name, k in told.items():
-        if not any(x in name for x in SPILLS):
-            assert field(k, "private_segment_fixed_size") == 0, name
+        assert field(k, "private_segment_fixed_size") == 0, name
     for part, waves in WAVES.get(source, {}).items():
         instances = [field(k, "vgpr_count") for n, k in told.items() if part in n]
         assert instances and max(instances) <= 512 // waves // 8 * 8, (part, instances)
