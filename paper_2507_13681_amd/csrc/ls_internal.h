@@ -255,15 +255,16 @@ struct PagedArgs {
 };
 
 // ls_packed_prefill.  An item is a block of 128 rows of one KV head of one sequence, where a "row" is one of the G query heads of one query: row r is head r % G of query
-// r / G.  Items go by how many 32-key steps they take, the longest first; where there are few of them they are cut into parts of `length` steps.
+// r / G.  Items go by how many 32-key steps they take; where there are few of them they are cut into parts.  (Keys, and queries times G, are less than 2^31: 32-bit divisions,
+// which take a tenth of the instructions that 64-bit ones do.)
 constexpr int PACKED_ROWS = 128, PACKED_KEYS = 32;
 struct PackedSeq { int keys, queries; };
-__host__ __device__ inline int packed_blocks(int queries, int G) { return (int)(((int64_t)queries * G + PACKED_ROWS - 1) / PACKED_ROWS); }
+__host__ __device__ inline int packed_blocks(int queries, int G) { return (int)(((uint32_t)queries * (uint32_t)G + (PACKED_ROWS - 1)) / PACKED_ROWS); }
 // steps that block j of a sequence takes: those up to the last key that its last row sees
 __host__ __device__ inline int packed_steps(const PackedSeq& s, int G, int j) {
-    const int64_t rows = (int64_t)s.queries * G, end = (int64_t)PACKED_ROWS * (j + 1) < rows ? (int64_t)PACKED_ROWS * (j + 1) : rows;
-    const int64_t seen = (int64_t)s.keys - s.queries + (end - 1) / G + 1;
-    return seen > 0 ? (int)((seen + PACKED_KEYS - 1) / PACKED_KEYS) : 0;
+    const uint32_t rows = (uint32_t)s.queries * (uint32_t)G, behind = (uint32_t)PACKED_ROWS * (uint32_t)(j + 1), end = behind < rows ? behind : rows;
+    const int seen = s.keys - s.queries + (int)((end - 1) / (uint32_t)G) + 1;
+    return seen > 0 ? (int)(((uint32_t)seen + (PACKED_KEYS - 1)) / PACKED_KEYS) : 0;
 }
 // blocks of a sequence that take more than x steps: its last ones.  (The last row sees query y or one after it, y = 32 x - keys + queries, if
 // the block ends behind row y G.)
@@ -272,7 +273,7 @@ __host__ __device__ inline int packed_longer(const PackedSeq& s, int G, int x) {
     if (x < 0) return blocks;
     const int64_t y = (int64_t)PACKED_KEYS * x - s.keys + s.queries;
     if (y >= s.queries) return 0;
-    return y <= 0 ? blocks : blocks - (int)(y * G / PACKED_ROWS);
+    return y <= 0 ? blocks : blocks - (int)((uint32_t)y * (uint32_t)G / PACKED_ROWS);
 }
 // no less than the steps of all its blocks together (each less than 4 above what is linear in j)
 __host__ __device__ inline float packed_work(const PackedSeq& s, int G) {
@@ -310,7 +311,7 @@ struct PackedArgs {
     int n, n_hat;
     float scale_log2e;
     PackedCut cut;
-    bool sorted;              // more items than workgroups are resident: the longest first
+    bool sorted;              // more items than workgroups are resident: those of the longest sequences first
     float *part_o, *part_ml;  // [units][128][d] accumulators in lane order, [units][128][2] reference and normaliser
     int32_t* status;
 };

@@ -8,8 +8,8 @@
 // Steps.  32 keys, from barrier to barrier: K and V rows of the next step go global -> LDS while S^T = K Q^T, softmax and O^T += V^T P^T of this one run, from two
 // buffers, by the 32x32 products of ls_device.h; bf16 V^T fragments come from the LDS transpose read.  No maximum is looked for on the way: the exponentials are
 // taken with the reference as it stands, and where a lane's sum exceeds a limit the step's softmax is done again with its maximum as the reference.
-// Items.  Which item a workgroup has follows from the starts, which only the device knows: a wave's lanes keep a sequence each, and count how many items take more than x steps
-// (packed_longer); a search over x finds the item of a rank, so the longest go first, whatever the lengths, and no launch ahead of this one has to put them in order.
+// Items.  Which item a workgroup has follows from the starts, which only the device knows: a wave's lanes keep a sequence each and add up their blocks, those of the longest
+// sequences first, the last block of each first; no launch ahead of this one puts them in order.
 #include <algorithm>
 #include <type_traits>
 #include "ls_device.h"
@@ -19,7 +19,7 @@ namespace ls {
 
 constexpr int PK_THREADS = 256;
 constexpr int PK_RING_S = 4, PK_RING_P = 2;      // fragments in flight ahead of the products of S, of P V
-constexpr float PK_LIMIT = 32.f, PK_FIRST = 4.f; // what a lane's probabilities of a step may sum to; in an item's first step
+constexpr float PK_LIMIT = 32.f;                 // what a lane's probabilities of a step may sum to
 
 template <typename T, int D>
 struct PackCfg {
@@ -45,8 +45,8 @@ __device__ __forceinline__ uint32_t lanes_sum(uint32_t x) { return (uint32_t)__b
 
 // The sequences, one a lane, and what a workgroup has of them
 struct PackedWork {
-    PackedSeq seq;            // of sequence `lane` (of 64 at a time)
-    int G, lane;
+    PackedSeq seq;            // of sequence `lane` (of 64 at a time), or `index`
+    int G, lane, index;
     // the item, its part, and the unit it is
     int s, block, part, length;
     bool stopped = false;     // a sequence before had starts that are none
@@ -69,22 +69,18 @@ struct PackedWork {
         stopped = stopped || none != 0ull;
     }
     __device__ int longer(int x) const { return (int)lanes_sum((uint32_t)packed_longer(seq, G, x)); }
-    // the item of rank r among those of a KV head, the longest first; false: there are not so many.  (At most 64 sequences.)
-    __device__ bool find(int r) {
-        if (r >= longer(-1)) return false;
-        int lo = -1, hi = longest() + 8;                   // rank r takes more than lo steps, and at most hi (a float has the longest, 2^26 at most, to within 4)
-        while (hi - lo > 1) {
-            const int x = (lo + hi) >> 1;
-            if (longer(x) <= r) hi = x; else lo = x;
+    // the sequences (at most 64) by their longest items
+    __device__ void sort(const PackedArgs& a) {
+        const int steps = seq.queries > 0 ? packed_steps(seq, G, packed_blocks(seq.queries, G) - 1) : -1;
+        if (__ballot(lane < a.B && steps != __builtin_amdgcn_readfirstlane(steps)) == 0ull) return;
+        int rank = lane < a.B ? 0 : lane;
+        for (int i = 0; i < a.B; ++i) {
+            const int o = __builtin_amdgcn_readlane(steps, i);
+            rank += lane < a.B && (o > steps || (o == steps && i < lane)) ? 1 : 0;
         }
-        // items of `hi` steps: each sequence has some neighbouring ones
-        const int above = packed_longer(seq, G, hi), mine = packed_longer(seq, G, hi - 1) - above;
-        const int upto = (int)lanes_upto((uint32_t)mine), at = r - (int)lanes_sum((uint32_t)above);
-        const uint64_t in = __ballot(at < upto);
-        s = __builtin_ctzll(in);
-        const int k = __builtin_amdgcn_readlane(upto, s) - 1 - at;              // how many of them follow in the sequence
-        block = packed_blocks(__builtin_amdgcn_readlane(seq.queries, s), G) - __builtin_amdgcn_readlane(above, s) - 1 - k;
-        return true;
+        seq.keys = __builtin_amdgcn_ds_permute(4 * rank, seq.keys);
+        seq.queries = __builtin_amdgcn_ds_permute(4 * rank, seq.queries);
+        index = __builtin_amdgcn_ds_permute(4 * rank, lane);
     }
     // by sequence, however many there are
     __device__ bool find_in_order(const PackedArgs& a, int r) {
@@ -95,7 +91,7 @@ struct PackedWork {
             const uint64_t in = __ballot(r < upto);
             if (in != 0ull) {
                 const int l = __builtin_ctzll(in);
-                s = s0 + l;
+                s = s0 + l;                                // (of a call that sorts them: the place)
                 block = __builtin_amdgcn_readlane(upto, l) - 1 - r;            // (the last of a sequence first)
                 return true;
             }
@@ -172,8 +168,10 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
         else if (a.Hkv % 8 == 0) { kvh = x + 8 * (i % (a.Hkv / 8)); rank = i / (a.Hkv / 8); }
         else { kvh = u % a.Hkv; rank = u / a.Hkv; }
     }
-    if (!(a.cut.units ? w.find_part(a, rank) : a.sorted ? w.find(rank) : w.find_in_order(a, rank))) return;
-    const int s = uniform(w.s), block = uniform(w.block), sl64 = s & 63;
+    w.index = lane;
+    if (a.sorted) w.sort(a);
+    if (!(a.cut.units ? w.find_part(a, rank) : w.find_in_order(a, rank))) return;
+    const int sl64 = uniform(w.s) & 63, s = a.sorted ? __builtin_amdgcn_readlane(w.index, sl64) : uniform(w.s), block = uniform(w.block);
     const int nk = __builtin_amdgcn_readlane(w.seq.keys, sl64), nq = __builtin_amdgcn_readlane(w.seq.queries, sl64);
     const int64_t q0 = a.q_starts ? a.q_starts[s] : 0, k0 = a.k_starts ? a.k_starts[s] : 0, pad = a.q_starts ? 0 : s;
     const int steps = packed_steps(PackedSeq{nk, nq}, G, block);
@@ -312,7 +310,8 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
 #pragma unroll
         for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
     const float sc2 = a.scale_log2e;
-    float mneg = INFINITY, l_run = 0.f, limit = PK_FIRST;  // the softmax reference of this lane's row in base 2, negated (+inf: no key seen yet); its share of the normaliser
+    int fresh = 1;
+    float mneg = INFINITY, l_run = 0.f;  // the softmax reference of this lane's row in base 2, negated (+inf: no key seen yet); its share of the normaliser
     constexpr int NS = C::KSTEPS, NV = 2 * C::DBLK;
     constexpr int RS = PK_RING_S < NS ? PK_RING_S : NS, RV = PK_RING_P;
     auto process = [&](auto SENDS, int h) {
@@ -343,15 +342,20 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
 #pragma unroll
         for (int k = 0; k < RV; ++k) vload(vf[k], base, k);                      // ahead of the softmax
         Probs pr;
-        float sum0 = 0.f, sum1 = 0.f;
+        float sum = 0.f;
+        int again = fresh;                                 // (the first step of a part has no reference yet)
+        if (!again) {
+            float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; r += 2) {
-            const float e0 = fast_exp2(__builtin_fmaf(x[r], sc2, mneg)), e1 = fast_exp2(__builtin_fmaf(x[r + 1], sc2, mneg));
-            sum0 += e0; sum1 += e1;
-            pr.set(r, e0, e1);
+            for (int r = 0; r < 16; r += 2) {
+                const float e0 = fast_exp2(__builtin_fmaf(x[r], sc2, mneg)), e1 = fast_exp2(__builtin_fmaf(x[r + 1], sc2, mneg));
+                sum0 += e0; sum1 += e1;
+                pr.set(r, e0, e1);
+            }
+            sum = sum0 + sum1;
+            again = __ballot(!(sum <= PK_LIMIT)) != 0ull;
         }
-        float sum = sum0 + sum1;
-        if (__ballot(!(sum <= limit)) != 0ull) {           // once more, with a new reference
+        if (apart(again)) {                                // with a new reference
             float mx = -INFINITY;
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, x[r]);
@@ -375,7 +379,7 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
                 if (r % 4 == 2) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        limit = PK_LIMIT;
+        fresh = 0;
         l_run += sum;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -443,14 +447,16 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
     __builtin_amdgcn_wave_barrier();
     unsigned char* og = a.out.data + (pad * a.out.seq + q0 * a.out.row + (int64_t)kvh * G * a.out.head) * Elem<T>::bytes;
     const int cr = lane / C::DS, cs = lane % C::DS;
+    // the query and head of the lane's row, and from one store to the next RPI rows on
+    uint32_t i = (uint32_t)(rho0 + cr) / (uint32_t)G, e = (uint32_t)(rho0 + cr) - i * (uint32_t)G;
+    const uint32_t more_i = (uint32_t)C::RPI / (uint32_t)G, more_e = (uint32_t)C::RPI % (uint32_t)G;
 #pragma unroll
     for (int j = 0; j < 32 / C::RPI; ++j) {
         const int r = C::RPI * j + cr;
         const f32x4 y = *reinterpret_cast<const f32x4*>(ow + r * C::OUT_ROW + 16 * cs);
-        if (rho0 + r < rows) {
-            const int64_t i = (uint32_t)(rho0 + r) / (uint32_t)G, e = rho0 + r - i * G;
-            *reinterpret_cast<f32x4*>(og + (i * a.out.row + e * a.out.head) * Elem<T>::bytes + 16 * cs) = y;
-        }
+        if (rho0 + r < rows) *reinterpret_cast<f32x4*>(og + ((int64_t)i * a.out.row + (int64_t)e * a.out.head) * Elem<T>::bytes + 16 * cs) = y;
+        i += more_i; e += more_e;
+        if (e >= (uint32_t)G) { e -= (uint32_t)G; ++i; }
     }
 }
 
