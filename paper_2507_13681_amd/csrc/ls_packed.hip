@@ -184,7 +184,6 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
     const bool on = rho < rows;
     const int qi = (int)((on ? (uint32_t)rho : 0u) / (uint32_t)G), hd = kvh * G + (int)(on ? (uint32_t)rho : 0u) - qi * G;
     const uint32_t rho_end = (uint32_t)(rho0 + 31 < rows ? rho0 + 31 : rows - 1);
-    const int pos_least = rows_here ? nk - nq + uniform((int)((uint32_t)rho0 / (uint32_t)G)) : 0;
     const int pos_most = rows_here ? nk - nq + uniform((int)(rho_end / (uint32_t)G)) : -1;
     const int pos = on ? nk - nq + qi : pos_most;          // last key that this lane's row sees (one that does not exist has zeros for a query, and finite results)
 
@@ -314,8 +313,60 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
     float mneg = INFINITY, l_run = 0.f;  // the softmax reference of this lane's row in base 2, negated (+inf: no key seen yet); its share of the normaliser
     constexpr int NS = C::KSTEPS, NV = 2 * C::DBLK;
     constexpr int RS = PK_RING_S < NS ? PK_RING_S : NS, RV = PK_RING_P;
-    auto process = [&](auto SENDS, int h) {
+    // Where some rows do not see all of a step's keys, an infinity or NaN in V must not reach those with weight zero: they are taken out of the fragments (`odd`: there were any), ..
+    auto only_finite = [](Frag<T>& f, uint32_t& odd) {
+        if constexpr (C::F32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { const bool is = fabsf(f.v[e]) < INFINITY; odd |= is ? 0u : 1u; f.v[e] = is ? f.v[e] : 0.f; }
+        } else {
+            typedef __attribute__((ext_vector_type(2))) short s16x2;
+            struct U { uint32_t w[4]; } u = __builtin_bit_cast(U, f.v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {                  // an exponent of ones carries into the sign
+                const s16x2 up = (__builtin_bit_cast(s16x2, u.w[e] & 0x7F807F80u) + s16x2{0x80, 0x80}) >> 15;
+                const uint32_t is = __builtin_bit_cast(uint32_t, up);
+                odd |= is;
+                u.w[e] &= ~is;
+            }
+            f.v = __builtin_bit_cast(bf16x8, u);
+        }
+    };
+    // .. and what a row sees of them is added by its kind: how many of each it sees is one more product
+    auto ones = [](auto is) {                              // a fragment of ones and zeros
+        Frag<T> f;
+        if constexpr (C::F32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f.v[e] = is(e) ? 1.f : 0.f;
+        } else {
+            struct U { uint32_t w[4]; } u;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { u.w[e] = (is(2 * e) ? 0x3F80u : 0u) | (is(2 * e + 1) ? 0x3F800000u : 0u); asm volatile("" : "+v"(u.w[e])); }
+            f.v = __builtin_bit_cast(bf16x8, u);
+        }
+        return f;
+    };
+    auto add_odd = [&](const unsigned char* base, int last) {                // last: key of the step that the lane's row sees at most
+#pragma unroll
+        for (int i = 0; i < C::DBLK; ++i)
+#pragma unroll 1
+            for (int kind = 0; kind < 3; ++kind) {         // +inf, -inf, NaN
+                const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+                f32x16 c = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    Frag<T> f;
+                    vload(f, base, half * C::DBLK + i);
+                    f = ones([&](int e) { const float x = (float)f.v[e]; return kind < 2 ? x == what : x != x; });
+                    mma(c, f, ones([&](int e) { return 16 * half + 8 * (e / 4) + 4 * g + e % 4 <= last; }));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int r = 0; r < 16; ++r) oacc[i][r] += c[r] > 0.f ? what : 0.f;
+            }
+    };
+    auto process = [&](auto SENDS, auto MASKED, int h) {
         constexpr int SN = decltype(SENDS)::value;
+        constexpr bool masked = decltype(MASKED)::value;
         const unsigned char* base = pk_lds + (h & 1) * C::STEP_BYTES;
         f32x16 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         Frag<T> kf[NS];
@@ -332,8 +383,7 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        if (PACKED_KEYS * h + PACKED_KEYS - 1 > pos_least) {
-            asm volatile("");                              // (few steps: a branch, no selects in the others)
+        if constexpr (masked) {
             const int lim = pos - PACKED_KEYS * h - 4 * g;
 #pragma unroll
             for (int r = 0; r < 16; ++r) x[r] = 8 * (r / 4) + r % 4 <= lim ? x[r] : -INFINITY;
@@ -343,8 +393,8 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
         for (int k = 0; k < RV; ++k) vload(vf[k], base, k);                      // ahead of the softmax
         Probs pr;
         float sum = 0.f;
-        int again = fresh;                                 // (the first step of a part has no reference yet)
-        if (!again) {
+        uint64_t again = fresh ? ~0ull : 0ull;             // lanes whose reference has to move (the first step of a part has none yet)
+        if (!fresh) {
             float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
@@ -353,14 +403,14 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
                 pr.set(r, e0, e1);
             }
             sum = sum0 + sum1;
-            again = __ballot(!(sum <= PK_LIMIT)) != 0ull;
+            again = __ballot(!(sum <= PK_LIMIT));
         }
-        if (apart(again)) {                                // with a new reference
+        if (apart(again != 0ull)) {                        // with a new reference for their rows; the others' stays, so that no row's result depends on its neighbours'
             float mx = -INFINITY;
 #pragma unroll
             for (int r = 0; r < 16; ++r) mx = fmaxf(mx, x[r]);
             mx = fmaxf(mx, xor32(mx)) * sc2;
-            const float m_new = fmaxf(mx, -mneg);
+            const float m_new = (again >> r32 | again >> (r32 + 32)) & 1ull ? fmaxf(mx, -mneg) : -mneg;
             const bool seen = m_new > -INFINITY;
             const float corr = seen ? fast_exp2(-mneg - m_new) : 1.f, safe = seen ? -m_new : 0.f;
             mneg = -m_new;
@@ -382,11 +432,16 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
         fresh = 0;
         l_run += sum;
         __builtin_amdgcn_sched_barrier(0);
+        uint32_t odd = 0u;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
+            if constexpr (masked) only_finite(vf[k], odd);
             mma(oacc[k % C::DBLK], vf[k], pr.frag(k / C::DBLK));
             if (k + RV < NV) vload(vf[k + RV], base, k + RV);
             __builtin_amdgcn_sched_barrier(0);
+        }
+        if constexpr (masked) {
+            if (apart(__ballot(odd != 0u) != 0ull)) add_odd(base, pos - PACKED_KEYS * h);
         }
     };
 
@@ -395,13 +450,13 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
         wait_transfers();
         __syncthreads();
         int h = h0;
-        // as long as the next step lies inside the keys its transfers go out between the products of this one
-        const int whole = nk / PACKED_KEYS - 1 < h1 - 1 ? nk / PACKED_KEYS - 1 : h1 - 1;
-        for (; h < whole; ++h) {
+        // As long as all rows of the workgroup see all keys of a step, and the next step lies inside the keys, whose transfers go out between the products of this one
+        const int least = nk - nq + uniform((int)((uint32_t)(PACKED_ROWS * block) / (uint32_t)G)), clear = least < 0 ? 0 : (least + 1) / PACKED_KEYS;
+        const int inside = (nk / PACKED_KEYS < h1 ? nk / PACKED_KEYS : h1) - 1, plain = clear < inside ? clear : inside;
+        for (; h < plain; ++h) {
             aim(h + 1);
-            const int active = PACKED_KEYS * h <= pos_most;
-            if (active) process(std::integral_constant<int, 2 * C::IPW>{}, h);
-            if (apart(active) == 0) {
+            if (rows_here) process(std::integral_constant<int, 2 * C::IPW>{}, std::false_type{}, h);
+            if (apart(rows_here) == 0) {
 #pragma unroll
                 for (int i = 0; i < 2 * C::IPW; ++i) send(i);
             }
@@ -410,7 +465,7 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
         }
         for (; h < h1; ++h) {
             if (h + 1 < h1) fetch(h + 1);
-            if (PACKED_KEYS * h <= pos_most) process(std::integral_constant<int, 0>{}, h);
+            if (PACKED_KEYS * h <= pos_most) process(std::integral_constant<int, 0>{}, std::true_type{}, h);
             wait_transfers();
             __syncthreads();
         }

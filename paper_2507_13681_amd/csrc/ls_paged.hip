@@ -37,7 +37,7 @@ struct PagedCfg {
     static constexpr int PS = D + 4;                      // floats of a partial result: output, reference, normaliser, 2 unused
     // slot swizzle of the staged V rows (XOR on the 16-byte slot index): the rows a transpose read touches fall into different banks
     __device__ static constexpr int vswz(int row) {
-        if (E4M3) return D == 128 ? (row & 7) : ((row >> 1) & 3);
+        if (E4M3) return D == 128 ? ((row ^ row >> 4) & 7) : ((row >> 1 ^ (row >> 4 & 1)) & 3);
         return D == 128 ? 2 * (row & 7) : 2 * ((row >> 1) & 3);
     }
 };

@@ -261,3 +261,66 @@ def test_what_the_binding_refuses():
             ctx.ls_packed_prefill(shape, **a)
     with pytest.raises(binding.LoopServeError):            # rows of an output that overlap
         ctx.ls_packed_prefill(shape, q, k, v, st, st, out[:1].expand(40, 4, 64))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("Hq,Hkv,d,n,at,dtype", [
+    (4, 4, 128, 200, 101, torch.bfloat16), (8, 2, 128, 300, 150, torch.bfloat16), (4, 2, 64, 130, 64, torch.bfloat16), (32, 1, 64, 70, 33, torch.bfloat16),
+    (4, 2, 128, 100, 37, torch.float32), (4, 1, 64, 90, 31, torch.float32)])
+def test_what_a_row_does_not_see_does_not_reach_it(Hq, Hkv, d, n, at, dtype, bad):
+    """Keys and values from a position on are no numbers: the rows before it have the same bits as with numbers there."""
+    q, k, v = _inputs(21, Hq, Hkv, d, [n], [n], dtype)
+    print("packed future", Hq, Hkv, d, n, at, dtype, bad, flush=True)
+    out, lse = _run(q, k, v, [n], [n])
+    k2, v2 = k.clone(), v.clone()
+    k2[at:], v2[at:] = bad, bad
+    got, got_lse = _run(q, k2, v2, [n], [n])
+    assert torch.equal(got[:at], out[:at]) and torch.equal(got_lse[:, :at], lse[:, :at])
+    assert not torch.isfinite(got[at:]).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_values_that_are_not_finite_reach_those_who_see_them(dtype):
+    """Single infinities and NaN in V: in their column of the output, from their position on, what the sum gives; in other columns and before, the same bits."""
+    n, d = 140, 64
+    q, k, v = _inputs(22, 4, 2, d, [n], [n], dtype, scale=0.5)
+    print("packed odd values", dtype, flush=True)
+    out, _ = _run(q, k, v, [n], [n])
+    v2 = v.clone()
+    places = {(50, 0, 3): float("inf"), (90, 0, 3): -float("inf"), (131, 1, 40): float("nan"), (139, 1, 63): -float("inf"), (0, 0, 10): float("inf")}
+    for (r, h, c), x in places.items():
+        v2[r, h, c] = x
+    got, _ = _run(q, k, v2, [n], [n])
+    want = out.double().clone()
+    for (r, h, c), x in places.items():
+        want[r:, 2 * h:2 * h + 2, c] += x
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    fine = torch.isfinite(want)
+    assert torch.equal(got[fine], out[fine]) and torch.equal(got[torch.isinf(want)].double(), want[torch.isinf(want)])
+
+
+def test_the_same_bits_every_time():
+    """Cut items and whole ones: parts are put together in one order."""
+    for keys, rows in (([5003, 900], [20, 30]), ([300, 77, 800], [300, 77, 800])):
+        q, k, v = _inputs(23, 8, 2, 128, keys, rows, torch.bfloat16)
+        print("packed bits", keys, flush=True)
+        first = _run(q, k, v, keys, rows)
+        for _ in range(3):
+            again = _run(q, k, v, keys, rows)
+            assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_rows_far_apart():
+    """Rows whose elements lie beyond 2^31 of the tensor."""
+    n, Hq, Hkv, d, step = 1200, 2, 1, 64, 1 << 21
+    q, k, v = _inputs(24, Hq, Hkv, d, [n], [n], torch.bfloat16)
+    whole = torch.zeros(n * step, dtype=torch.bfloat16, device="cuda")
+    rows = whole.view(n, step)
+    dk, dv, dq, out = (rows[:, a:a + w * d].unflatten(1, (w, d)) for a, w in ((0, Hkv), (1024, Hkv), (2048, Hq), (4096, Hq)))
+    dk.copy_(k), dv.copy_(v), dq.copy_(q)
+    shape = binding.make_shape(1, Hq, Hkv, d, n, n, 1, "bf16")
+    print("packed far apart", flush=True)
+    _context(shape).ls_packed_prefill(shape, dq, dk, dv, _starts([n]).cuda(), _starts([n]).cuda(), out)
+    torch.cuda.synchronize()
+    assert (n - 1) * step > 2 ** 31
+    _check(q, k, v, [n], [n], out.cpu().contiguous(), None)
