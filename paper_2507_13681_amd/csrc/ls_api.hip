@@ -27,11 +27,11 @@ struct ls_ctx {
     size_t ws_bytes;
     int32_t* status;          // device status word (bits LS_STAT_*), OR-ed into by kernels, read and cleared by ls_poll_status
     // [COUNTER_SETS][MAX_HEADS] workgroups finished per head or KV head inside a launch.  Set 0: ls_score, cleared by the call's
-    // first kernel.  The others take turns call by call in ls_decode_attend, one launch with nobody to clear a set ahead of it:
+    // first kernel.  The others take turns call by call in ls_decode_attend and ls_paged_attend, one launch with nobody to clear a set ahead of it:
     // a launch leaves zeros in its own and clears the one after the next.  So calls that overlapped against the rules, and left a
     // set off, spoil the next user of that set and no more.
     uint32_t* counters;
-    unsigned decode_calls;    // calls of ls_decode_attend that used a set
+    unsigned decode_calls;    // calls of those two that used a set
     int decode_heads;         // most KV heads of such a call: the part of a set that is cleared
     int walk_spin_limit;      // bound of the waits inside walk_kernel (test hook)
     char err[256];
@@ -44,7 +44,7 @@ struct ls_ctx {
 namespace {
 
 constexpr size_t ALIGN = 256;
-constexpr size_t MAX_HEADS = 65536;         // B * Hq (ls_score), B * Hkv (ls_decode_attend) <= 65535
+constexpr size_t MAX_HEADS = 65536;         // B * Hq (ls_score), B * Hkv (ls_decode_attend, ls_paged_attend) <= 65535
 constexpr unsigned DECODE_SETS = 4, COUNTER_SETS = 1 + DECODE_SETS;
 constexpr size_t COUNTER_BYTES = COUNTER_SETS * MAX_HEADS * sizeof(uint32_t);
 inline uint32_t* decode_set(const ls_ctx* c, unsigned call) { return c->counters + (1 + call % DECODE_SETS) * MAX_HEADS; }
@@ -743,7 +743,7 @@ Wrong check_paged(const ls_shape* s, const ls_cache* cache, const void* q, const
 Wrong check_packed_shape(const ls_shape* s) {
     const Wrong w = check_heads(s, true);
     if (w.code) return w;
-    if (s->n < 1 || s->n > MOST_ROWS || s->n_hat < 1 || s->n_hat * (s->Hq / s->Hkv) > MOST_ROWS) return {LS_ESHAPE, "n or n_hat out of range"};
+    if (s->n < 1 || s->n > MOST_ROWS || s->n_hat < 1 || s->n_hat > MOST_ROWS || s->n_hat * (s->Hq / s->Hkv) > MOST_ROWS) return {LS_ESHAPE, "n or n_hat out of range"};
     return FINE;
 }
 Wrong check_packed(const ls_shape* s, const ls_rows* q, const ls_rows* k, const ls_rows* v, const int32_t* q_starts, const int32_t* k_starts,

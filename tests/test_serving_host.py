@@ -43,6 +43,7 @@ PACKED = [
     (dict(), 0), (dict(starts=False), 0),
     (dict(shape=dict(d=96)), ESHAPE), (dict(shape=dict(Hq=6)), ESHAPE), (dict(shape=dict(B=0)), ESHAPE), (dict(shape=dict(n=0)), ESHAPE),
     (dict(shape=dict(n_hat=0)), ESHAPE), (dict(shape=dict(n_hat=2 ** 31)), ESHAPE), (dict(shape=dict(n_hat=2 ** 30 + 9)), ESHAPE),
+    (dict(shape=dict(n_hat=2 ** 62, Hq=16)), ESHAPE),       # times the query heads of a KV head it is 2^64
     (dict(shape=dict(B=9000)), ESHAPE), (dict(q=_rows(data=None)), EINVAL), (dict(q=None), EINVAL), (dict(k=_rows(data=HERE + 8)), EINVAL),
     (dict(v=_rows(row=516)), EINVAL), (dict(v=_rows(head=-128)), ESHAPE), (dict(k=_rows(row=2 ** 26)), ESHAPE), (dict(q=_rows(row=2 ** 58)), ESHAPE),
     (dict(out=_rows(row=512, head=128)), ESHAPE),           # eight heads in the room of four
