@@ -5,7 +5,7 @@
  *
  * Conventions for every entry point
  *   - All tensor pointers are DEVICE pointers on the context's GPU, 16-byte aligned, row-major and
- *     contiguous in the stated shape.  Only ls_shape and scalars are host data.
+ *     contiguous in the stated shape (ls_rows: of the strides it states).  Only the structures and scalars are host data.
  *   - The caller owns every tensor.  The library owns only the context and its workspace, which is
  *     allocated once in ls_create; no entry point below allocates or frees device memory.
  *   - Calls are asynchronous on `hip_stream` (a hipStream_t, NULL = the default stream) and contain
@@ -14,9 +14,9 @@
  *     a host round trip.  Calls that share a context must be issued on one stream at a time (they
  *     share the workspace, and counters through which the workgroups of a launch find out which of them
  *     is the last).  Calls that overlap all the same spoil their own results, and may leave those
- *     counters off for one or two later calls of ls_decode_attend on that context; the ones after
+ *     counters off for one or two later calls of ls_decode_attend or ls_paged_attend on that context; the ones after
  *     that are sound again.  A recorded call (HIP graph) always uses the same counters: replays that
- *     overlapped leave it unsound until three other calls of ls_decode_attend have run.
+ *     overlapped leave it unsound until three other calls of these two have run.
  *   - Return value: LS_OK or a negative ls_status; ls_last_error(ctx) then describes the failure.
  *     Argument errors are detected on the host before anything is launched.
  *   - dtype is the storage type of q / k / v / out (bf16 or fp32); tile products accumulate in fp32
@@ -292,7 +292,7 @@ typedef struct {
  *        none where that is negative.  A sequence whose starts descend or leave [0, n] or [0, n_hat] is passed by, with
  *        all behind it (LS_STAT_STARTS).
  * Outputs:
- *   out in dtype; a row that sees no key is all zeros.  Rows of no sequence stay as they are.
+ *   out in dtype; a row that sees no key is all zeros, and one that sees a NaN logit is NaN, with its lse.  Rows of no sequence stay as they are.
  *   lse fp32 or NULL, [Hq,n_hat] (packed) or [B,Hq,n_hat]: natural log of the softmax denominator (-inf without a key)
  * Workspace: ls_packed_workspace_bytes (0 for an invalid shape); less is enough where the rows fill the chip, and slower elsewhere.
  */
@@ -331,7 +331,7 @@ int ls_cache_read(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, con
  *        page)], with LS_STAT_PAGE_RANGE where that is less than len).  n_hat, w are ignored.  Hq/Hkv <= 32.
  *   q [B,Hq,d];  table [B,max_pages], len [B] int32, device memory
  * Outputs:
- *   out [B,Hq,d] in dtype; all zeros where there is no key
+ *   out [B,Hq,d] in dtype; all zeros where there is no key, NaN (and so the lse) where a logit is
  *   lse [B,Hq] fp32 or NULL: natural log of the softmax denominator (-inf when there is no key)
  * Workspace: ls_paged_workspace_bytes (0 for an invalid shape).  What this header says of calls of ls_decode_attend that overlap holds for
  * these too: they share its counters.

@@ -8,6 +8,7 @@
 // Steps.  32 keys, from barrier to barrier: K and V rows of the next step go global -> LDS while S^T = K Q^T, softmax and O^T += V^T P^T of this one run, from two
 // buffers, by the 32x32 products of ls_device.h; bf16 V^T fragments come from the LDS transpose read.  No maximum is looked for on the way: the exponentials are
 // taken with the reference as it stands, and where a lane's sum exceeds a limit the step's softmax is done again with its maximum as the reference.
+// What a row does not see weighs nothing, whatever it holds, and a row's reference moves for that row alone: its result has the same bits whatever its neighbours are.
 // Items.  Which item a workgroup has follows from the starts, which only the device knows: a wave's lanes keep a sequence each and add up their blocks, those of the longest
 // sequences first, the last block of each first; no launch ahead of this one puts them in order.
 #include <algorithm>
@@ -99,19 +100,18 @@ struct PackedWork {
         }
         return false;
     }
-    // steps of a part of a call that cuts its items
-    __device__ int longest() const {                       // steps of the longest item
+    __device__ int longest() const {                       // steps of the longest item, or nearly (a float)
         const float most = seq.queries > 0 ? (float)packed_steps(seq, G, packed_blocks(seq.queries, G) - 1) : 0.f;
         return __builtin_amdgcn_readfirstlane((int)wave_largest(most));
     }
-    __device__ void cut_length(const PackedArgs& a) {
+    __device__ void cut_length(const PackedArgs& a) {      // steps of a part, of a call that cuts its items
         length = __builtin_amdgcn_readfirstlane(packed_length(a.cut, a.Hkv, wave_sum(packed_work(seq, G)), longer(-1), longest()));
     }
     __device__ int longer_than_part(const PackedSeq& x, int p) const {          // blocks that have a part p
         const int64_t steps = (int64_t)p * length;
         return p == 0 ? packed_longer(x, G, -1) : steps > 1 << 28 ? 0 : packed_longer(x, G, (int)steps);
     }
-    // blocks that have a part p0 + lane, of sequences 0 .. most - 1 (with `before`: of those before sequence `stop`)
+    // blocks that have a part p0 + lane (and in *before those of the sequences before `stop`)
     __device__ int having(const PackedArgs& a, int p0, int stop = 0, int* before = nullptr) const {
         int sum = 0;
         for (int i = 0; i < a.B; ++i) {
@@ -121,7 +121,7 @@ struct PackedWork {
         }
         return sum;
     }
-    // Units of a KV head in the order of parts, and those by sequence and block: unit r is ..  (All run at once, so that their order does not matter.)
+    // Units of a KV head go by part, those of a part by sequence, the last block of each first: unit r is ..  (All run at once, so that the order does not matter.)
     __device__ bool find_part(const PackedArgs& a, int r) {
         cut_length(a);
         int before = 0;
@@ -484,10 +484,10 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
         return;
     }
     if (!rows_here) return;
-    const float inv = l_tot > 0.f ? 1.0f / l_tot : 0.f;
+    const float inv = l_tot != 0.f ? 1.0f / l_tot : 0.f;                     // 0 without a key, NaN where a logit is
     if (a.lse && g == 0 && on)
         a.lse[(a.q_starts ? (int64_t)hd * a.n_hat + q0 : ((int64_t)s * a.Hq + hd) * a.n_hat) + qi] =
-            l_tot > 0.f ? (log2f(l_tot) - mneg) * 0.69314718055994531f : -INFINITY;
+            l_tot != 0.f ? (log2f(l_tot) - mneg) * 0.69314718055994531f : -INFINITY;
     // A lane holds four neighbouring values of its row at a time; through LDS (32 rows of this wave in the buffers, which nobody reads any more) they become whole rows
     unsigned char* ow = pk_lds + wv * (32 * C::OUT_ROW);
 #pragma unroll
@@ -609,12 +609,12 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
     if (rho0 + r32 >= rows) continue;
     const int64_t rho = rho0 + r32, qi = (uint32_t)rho / (uint32_t)G, hd = kvh * (int64_t)G + (rho - qi * G);
     const int64_t q0 = a.q_starts ? a.q_starts[s] : 0, pad = a.q_starts ? 0 : s;
-    y *= L > 0.f ? 1.0f / L : 0.f;
+    y *= L != 0.f ? 1.0f / L : 0.f;
     unsigned char* dst = a.out.data + (pad * a.out.seq + (q0 + qi) * a.out.row + hd * a.out.head + 32 * i + 8 * sub + 4 * g) * Elem<T>::bytes;
     if constexpr (C::F32) *reinterpret_cast<f32x4*>(dst) = y;
     else *reinterpret_cast<__attribute__((ext_vector_type(4))) __bf16*>(dst) = __builtin_convertvector(y, __attribute__((ext_vector_type(4))) __bf16);
     if (a.lse && i == 0 && sub == 0 && g == 0)
-        a.lse[(a.q_starts ? hd * a.n_hat + q0 : ((int64_t)s * a.Hq + hd) * a.n_hat) + qi] = L > 0.f ? (log2f(L) + top) * 0.69314718055994531f : -INFINITY;
+        a.lse[(a.q_starts ? hd * a.n_hat + q0 : ((int64_t)s * a.Hq + hd) * a.n_hat) + qi] = L != 0.f ? (log2f(L) + top) * 0.69314718055994531f : -INFINITY;
     }
 }
 

@@ -337,9 +337,9 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
     __syncthreads();
     bf16_t* out = reinterpret_cast<bf16_t*>(a.out) + ((int64_t)b * a.Hq + kvh * G) * D;
     float* lse = a.lse ? a.lse + (int64_t)b * a.Hq + kvh * G : nullptr;
-    auto finish = [&](int head, int dd, float m, float o0, float o1, float l) {   // two output elements (dd == 0 also writes lse)
-        *reinterpret_cast<uint32_t*>(out + head * D + dd) = (uint32_t)f2bf(l > 0.f ? o0 / l : 0.f) | ((uint32_t)f2bf(l > 0.f ? o1 / l : 0.f) << 16);
-        if (lse && dd == 0) lse[head] = l > 0.f ? (m * sc2 + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    auto finish = [&](int head, int dd, float m, float o0, float o1, float l) {   // two output elements (dd == 0 also writes lse); l: 0 without a key, NaN where a logit is
+        *reinterpret_cast<uint32_t*>(out + head * D + dd) = (uint32_t)f2bf(l != 0.f ? o0 / l : 0.f) | ((uint32_t)f2bf(l != 0.f ? o1 / l : 0.f) << 16);
+        if (lse && dd == 0) lse[head] = l != 0.f ? (m * sc2 + log2f(l)) * 0.69314718055994531f : -INFINITY;
     };
     float* shared_part = a.part + (int64_t)w.base * G * PS;           // [part][head][PS]
     const int items = G * (D / 2);                                     // two neighbouring elements of a head
@@ -414,8 +414,8 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
 #pragma unroll
             for (int e = 0; e < PG_BATCH; ++e) {
                 const int s = s0 + e * subs;
-                if (s < cuts && mh[s].x > -INFINITY) {
-                    const float wgt = fast_exp2((mh[s].x - m) * sc2);
+                if (s < cuts) {
+                    const float wgt = mh[s].x > -INFINITY ? fast_exp2((mh[s].x - m) * sc2) : 0.f;        // (NaN times 0 stays NaN)
                     o0 += x[e].x * wgt; o1 += x[e].y * wgt;
                     l += mh[s].y * wgt;
                 }
@@ -474,9 +474,9 @@ __global__ __launch_bounds__(2 * D) void paged_join_kernel(PagedArgs a) {
         const float2 x = red[u][tid % LANES];
         o0 += x.x * wgt; o1 += x.y * wgt; l += red[u][LANES].x * wgt;
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
     reinterpret_cast<uint32_t*>(reinterpret_cast<bf16_t*>(a.out) + (int64_t)blockIdx.x * D)[dd / 2] = (uint32_t)f2bf(o0 * inv) | ((uint32_t)f2bf(o1 * inv) << 16);
-    if (a.lse && dd == 0) a.lse[blockIdx.x] = l > 0.f ? (m * a.scale_log2e + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    if (a.lse && dd == 0) a.lse[blockIdx.x] = l != 0.f ? (m * a.scale_log2e + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
 // A head's tiles are at most all there are, and a part no shorter than these by the slots: t / paged_length(..) <= slots / Hkv, whatever t is.

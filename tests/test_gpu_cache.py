@@ -327,6 +327,32 @@ def test_pages_that_are_nowhere(kind):
     assert status == 0 and (out == 0).all() and torch.isneginf(lse).all()
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lens,Hq,Hkv,d,first,last", [
+    ([70, 70], 8, 2, 128, 40, 41),                   # one workgroup a head
+    ([70, 70], 8, 2, 64, 0, 70),                     # no other key
+    ([5003], 32, 1, 64, 100, 101),                   # parts, put together by a launch of their own
+    ([5003], 32, 1, 64, 0, 3000),                    # parts that have no other key
+    ([2000, 2000], 4, 2, 128, 1999, 2000),           # parts, put together by the last of them
+    ([2000, 2000], 4, 2, 128, 0, 1500)])
+def test_no_number_that_is_seen_stays_none(lens, Hq, Hkv, d, first, last, kind):
+    """NaN keys first .. last - 1 in head 0 of sequence 0: so are its heads' results; all others have the same bits as with numbers there."""
+    print("paged NaN", lens, Hq, Hkv, d, first, last, kind, flush=True)
+    rng = np.random.default_rng(17)
+    pages = sum(-(-n // 16) for n in lens)
+    p = pu.pool(rng, pages, Hkv, 16, d, kind)
+    q, table = pu.rnd(rng, len(lens), Hq, d), pu.table_for(rng, lens, 16, pages)
+    out, lse, _ = _attend(p, q, table, lens)
+    at = torch.arange(first, last)
+    p["k"][table[0, at // 16].long(), 0, at % 16] = float("nan") if kind == "bf16" else 0x7F
+    got, got_lse, status = _attend(p, q, table, lens, times=2)
+    assert status == 0
+    hit = torch.zeros(out.shape[:2], dtype=torch.bool)
+    hit[0, :Hq // Hkv] = True
+    assert torch.isnan(got[hit]).all() and torch.isnan(got_lse[hit]).all()
+    assert torch.equal(got[~hit], out[~hit]) and torch.equal(got_lse[~hit], lse[~hit])
+
+
 def test_shared_pages_no_lse_and_scale():
     """Two sequences with the same first pages, and no normaliser asked for."""
     rng = np.random.default_rng(11)

@@ -280,6 +280,21 @@ def test_what_a_row_does_not_see_does_not_reach_it(Hq, Hkv, d, n, at, dtype, bad
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Hq,Hkv,keys,rows,at", [(4, 2, 200, 200, 60), (4, 2, 200, 200, 0), (2, 1, 4000, 20, 0), (2, 1, 4000, 20, 3970), (2, 1, 4000, 4000, 1000)])
+def test_no_number_that_is_seen_stays_none(Hq, Hkv, keys, rows, at, dtype):
+    """A NaN key of head 0: the output and the normaliser of its heads' rows that see it are none either, whole items and parts; what else there is keeps its bits."""
+    q, k, v = _inputs(23, Hq, Hkv, 128, [keys], [rows], dtype)
+    print("packed NaN", Hq, Hkv, keys, rows, at, dtype, flush=True)
+    out, lse = _run(q, k, v, [keys], [rows])
+    k[at, 0] = float("nan")
+    got, got_lse = _run(q, k, v, [keys], [rows])
+    hit = torch.zeros(rows, Hq, dtype=torch.bool)
+    hit[max(0, at - (keys - rows)):, :Hq // Hkv] = True
+    assert torch.isnan(got[hit]).all() and torch.isnan(got_lse.T[hit]).all()
+    assert torch.equal(got[~hit], out[~hit]) and torch.equal(got_lse.T[~hit], lse.T[~hit])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_values_that_are_not_finite_reach_those_who_see_them(dtype):
     """Single infinities and NaN in V: in their column of the output, from their position on, what the sum gives; in other columns and before, the same bits."""
     n, d = 140, 64
