@@ -5,7 +5,8 @@
 // only rounding is that of the code, a stored value times its power is a bf16, and the attention over it needs no scaled products; what it costs is at most one of the
 // fifteen binades of e4m3 below a row's largest value.
 //
-// Bound by memory: each row is read and written once, and of each position the table's entry.
+// Bound by memory: each row is read and written once, and of each position the table's entry.  8 KV heads of 128, e4m3, us: 32768 bf16 rows written 43 (4.7 TB/s, read and written), four caches of
+// 16384 read back 81 (5.0 TB/s; a copy of 1 GiB reaches 5.15); one row of each of four sequences written 4.6, where an empty launch is 2.6.
 #include <type_traits>
 #include "ls_device.h"
 #include "ls_internal.h"
@@ -180,7 +181,8 @@ static hipError_t run_move_t(MoveArgs a, hipStream_t st) {
     constexpr int ROWS = MOVE_THREADS / (D / 8);
     const int64_t rows = (a.starts ? 1 : (int64_t)a.B) * a.n_hat;
     const int64_t blocks = (rows + ROWS - 1) / ROWS;
-    // all heads of a row in one workgroup where there are rows enough, few of them otherwise
+    // All heads of a row in one workgroup where there are rows enough: what a row is and where it goes is found once for them.  Two heads of them otherwise, for more workgroups.  All heads / two, us:
+    // four caches of 16384, packed 81 / 86, padded 81 / 79, 16384 rows of 32 heads of 64 49 / 51, four single rows 5.5 / 4.7, 3400 rows of fp32 5.8 / 5.4.
     a.heads = a.cache.Hkv;
     while (a.heads > 2 && blocks * ((a.cache.Hkv + a.heads - 1) / a.heads) < 2048) a.heads = (a.heads + 1) / 2;
     hipLaunchKernelGGL((move_kernel<WRITE, T, E4M3, D>), dim3((uint32_t)blocks, (a.cache.Hkv + a.heads - 1) / a.heads), dim3(MOVE_THREADS), 0, st, a);

@@ -206,13 +206,12 @@ struct MoveArgs {
 // knows.
 constexpr int PAGED_TILE = 32;               // keys
 // Few heads go in as many parts as there are compute units, which have a workgroup each; more heads, whose lengths may differ, in twice as many at most, two workgroups to a unit: what is
-// left over at the ends is shorter then, but a part more is a result more to put together.  256 parts / 512, us: four caches of 16384, 8 KV heads, e4m3 27.2 / 29.6, one of 131072, bf16 99 / 105; 13 caches of
-// 1 to 131072 112 / 106, 64 of 100 to 20000 115 / 104.  Parts are as short as lets all of them run at once (four caches of 500 to 60000, against the work by 256 and what the heads begin more in a
-// second round: 53 / 36 us, eight of 1000 to 30000 59 / 44).
+// left over at the ends is shorter then, but a part more is a result more to put together.  256 parts / 512, us: four caches of 16384, 8 KV heads, e4m3 31.1 / 33.6, one of 131072, bf16 96.7 / 102.2; 13 caches of
+// 1 to 67000 113.7 / 106.2, 24 of 0 to 31000 96 / 56.6.  Parts are as short as lets all of them run at once.
 constexpr int PAGED_ALONE = 64;              // heads up to which a workgroup has its compute unit for itself
 __host__ __device__ inline int paged_slots(int64_t heads) { return heads <= PAGED_ALONE ? 256 : 512; }
 __host__ __device__ inline bool paged_at_once(int64_t heads) { return heads * 4 <= paged_slots(heads) * 3; }
-// Tiles that a head is not cut for, two a wave: 17 tiles whole / in parts 9.5 / 8.6 us, 10 tiles 6.7 / 8.1
+// Tiles that a head is not cut for, two a wave.  Whole / in parts, us: 32 tiles 14.3 / 8.9, 17 tiles 9.8 / 8.7, 10 tiles 7.1 / 8.3, 16 tiles of 32 sequences 10.6 / 14.0
 constexpr int PAGED_WHOLE = 16;
 constexpr int PAGED_SHORTEST = 4, PAGED_SHORTEST_MANY = 32;                          // tiles of a part at least; of that many heads
 __host__ __device__ inline int paged_cuts(int tiles, int length) { return tiles <= PAGED_WHOLE ? 1 : (int)(((uint32_t)tiles + (uint32_t)length - 1) / (uint32_t)length); }
@@ -281,7 +280,8 @@ __host__ __device__ inline float packed_work(const PackedSeq& s, int G) {
     return blocks * (before + 4.f) + 0.5f * PACKED_ROWS / PACKED_KEYS * blocks * (blocks + 1.f) / (float)G;
 }
 constexpr int PACKED_SORTED = 64;            // with more sequences items go by sequence, whole
-// How a call cuts its items.  Parts are no more than the workgroups that are resident, so that they run at once.
+// How a call cuts its items.  Parts are no more than the workgroups that are resident, so that they run at once (fp32 at d = 128 twice as many: one and two rounds, us, 1024 positions 51.6 / 47.0,
+// 300 and 40 new rows behind 2700 and none 103.5 / 76.6).  Whole / cut, us: follow-ups of 1 to 200 rows on 2900 to 20000 keys 460 / 83, 61 new rows of 12347 216 / 37, fp32 1024 positions of 8 heads of 128 149 / 47.
 struct PackedCut {
     int units;                // parts that there is room for; 0: items are whole
     int least, some;          // steps of a part at least; up to this many, as many as leave a part to a compute unit
@@ -311,7 +311,7 @@ struct PackedArgs {
     int n, n_hat;
     float scale_log2e;
     PackedCut cut;
-    bool sorted;              // more items than workgroups are resident: those of the longest sequences first
+    int sorted;               // more items than workgroups are resident: how many are, and those of the longest sequences may go first; else 0
     float *part_o, *part_ml;  // [units][128][d] accumulators in lane order, [units][128][2] reference and normaliser
     int32_t* status;
 };

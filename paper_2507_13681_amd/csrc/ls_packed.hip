@@ -8,9 +8,11 @@
 // Steps.  32 keys, from barrier to barrier: K and V rows of the next step go global -> LDS while S^T = K Q^T, softmax and O^T += V^T P^T of this one run, from two
 // buffers, by the 32x32 products of ls_device.h; bf16 V^T fragments come from the LDS transpose read.  No maximum is looked for on the way: the exponentials are
 // taken with the reference as it stands, and where a lane's sum exceeds a limit the step's softmax is done again with its maximum as the reference.
+// One sequence of 32768, 32 query and 8 KV heads of 128, bf16: 7.2 to 7.6 ms by card (1.16 to 1.22 PFLOP/s; a library product of 16384^3 reaches 1.33); 32 of 700 188 us; fp32, 4 query heads of 64, 1024, 300 and 37: 22 us.
+// Three workgroups a CU at d = 128.  With queries of zeros, the same work, it takes 5.6 ms, and with the softmax left out 6.5: the clock under load counts for more than any one pipeline.
 // What a row does not see weighs nothing, whatever it holds, and a row's reference moves for that row alone: its result has the same bits whatever its neighbours are.
 // Items.  Which item a workgroup has follows from the starts, which only the device knows: a wave's lanes keep a sequence each and add up their blocks, those of the longest
-// sequences first, the last block of each first; no launch ahead of this one puts them in order.
+// sequences first where one is long beside the rest, the last block of each first; no launch ahead of this one puts them in order.
 #include <algorithm>
 #include <type_traits>
 #include "ls_device.h"
@@ -20,6 +22,9 @@ namespace ls {
 
 constexpr int PK_THREADS = 256;
 constexpr int PK_RING_S = 4, PK_RING_P = 2;      // fragments in flight ahead of the products of S, of P V
+// The longest item against the mean work of the workgroups that are resident at once, beyond which the sequences are sorted: at its end the call would wait for it.  Sorted / as they come, us, 4 or 8 KV
+// heads, the longest sequence the last: 0.15 times 1507 / 1483, 0.3 457 / 442, 0.7 562 / 546, 1.24 207 / 202, 1.27 245 / 277, 1.4 285 / 318, 1.9 177 / 228, 6.7 690 / 711; the first, 1.4 285 / 277.
+constexpr float PK_WAITS = 1.25f;
 constexpr float PK_LIMIT = 32.f;                 // what a lane's probabilities of a step may sum to
 
 template <typename T, int D>
@@ -70,8 +75,9 @@ struct PackedWork {
         stopped = stopped || none != 0ull;
     }
     __device__ int longer(int x) const { return (int)lanes_sum((uint32_t)packed_longer(seq, G, x)); }
-    // the sequences (at most 64) by their longest items
+    // the sequences (at most 64) by their longest items, where the longest of all takes so much of what a resident workgroup has to do that the call would wait for it
     __device__ void sort(const PackedArgs& a) {
+        if (!((float)longest() * (float)a.sorted > PK_WAITS * wave_sum(packed_work(seq, G)) * (float)a.Hkv)) return;
         const int steps = seq.queries > 0 ? packed_steps(seq, G, packed_blocks(seq.queries, G) - 1) : -1;
         if (__ballot(lane < a.B && steps != __builtin_amdgcn_readfirstlane(steps)) == 0ull) return;
         int rank = lane < a.B ? 0 : lane;
@@ -309,7 +315,6 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
 #pragma unroll
         for (int r = 0; r < 16; ++r) oacc[i][r] = 0.f;
     const float sc2 = a.scale_log2e;
-    int fresh = 1;
     float mneg = INFINITY, l_run = 0.f;  // the softmax reference of this lane's row in base 2, negated (+inf: no key seen yet); its share of the normaliser
     constexpr int NS = C::KSTEPS, NV = 2 * C::DBLK;
     constexpr int RS = PK_RING_S < NS ? PK_RING_S : NS, RV = PK_RING_P;
@@ -392,19 +397,15 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
 #pragma unroll
         for (int k = 0; k < RV; ++k) vload(vf[k], base, k);                      // ahead of the softmax
         Probs pr;
-        float sum = 0.f;
-        uint64_t again = fresh ? ~0ull : 0ull;             // lanes whose reference has to move (the first step of a part has none yet)
-        if (!fresh) {
-            float sum0 = 0.f, sum1 = 0.f;
+        float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
-            for (int r = 0; r < 16; r += 2) {
-                const float e0 = fast_exp2(__builtin_fmaf(x[r], sc2, mneg)), e1 = fast_exp2(__builtin_fmaf(x[r + 1], sc2, mneg));
-                sum0 += e0; sum1 += e1;
-                pr.set(r, e0, e1);
-            }
-            sum = sum0 + sum1;
-            again = __ballot(!(sum <= PK_LIMIT));
+        for (int r = 0; r < 16; r += 2) {
+            const float e0 = fast_exp2(__builtin_fmaf(x[r], sc2, mneg)), e1 = fast_exp2(__builtin_fmaf(x[r + 1], sc2, mneg));
+            sum0 += e0; sum1 += e1;
+            pr.set(r, e0, e1);
         }
+        float sum = sum0 + sum1;
+        const uint64_t again = __ballot(!(sum <= PK_LIMIT));                     // lanes whose reference has to move; without one yet the sum is infinite or none
         if (apart(again != 0ull)) {                        // with a new reference for their rows; the others' stays, so that no row's result depends on its neighbours'
             float mx = -INFINITY;
 #pragma unroll
@@ -429,7 +430,6 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
                 if (r % 4 == 2) __builtin_amdgcn_sched_barrier(0);
             }
         }
-        fresh = 0;
         l_run += sum;
         __builtin_amdgcn_sched_barrier(0);
         uint32_t odd = 0u;
@@ -630,7 +630,7 @@ PackedCut packed_cut(int B, bool packed, int64_t keys, int64_t queries, int Hkv,
     const int64_t units = (room < resident ? room : resident) / 8 * 8;
     if (units <= items || B > PACKED_SORTED) return c;
     c.units = (int)units;
-    // Where the host sees that nothing will be cut, there is no launch that looks for parts, 3 us: of equal sequences what the device finds, of others the least that it may find
+    // Where the host sees that nothing will be cut, there is no launch that looks for parts (an empty one is 2.6 us): of equal sequences what the device finds, of others the least that it may find
     const PackedSeq s{(int)keys, (int)queries};
     const int blocks = packed_blocks(s.queries, G), longest = packed_steps(s, G, blocks - 1);
     const bool whole = !packed || B == 1 ? packed_length(c, Hkv, packed_work(s, G) * (float)B, blocks * B, longest) == 1 << 28
@@ -643,7 +643,7 @@ template <typename T, int D>
 static hipError_t run_packed_t(PackedArgs a, hipStream_t st) {
     constexpr int dtype = PackCfg<T, D>::F32 ? 1 : 0;
     const int64_t items = packed_items(a.B, a.n_hat, a.Hkv, a.G, a.q_starts != nullptr);
-    a.sorted = a.B <= PACKED_SORTED && items > packed_resident(dtype, D);
+    a.sorted = a.B <= PACKED_SORTED && items > packed_resident(dtype, D) ? packed_resident(dtype, D) : 0;
     // the ranks of a KV head's items, rounded up to what the XCDs share
     int64_t groups = a.cut.units ? a.cut.units : (items + 7) / 8 * 8;
     if (!a.cut.units && 8 % a.Hkv != 0 && a.Hkv % 8 != 0) groups = items;

@@ -10,8 +10,8 @@
 //   e4m3: K codes become bf16 with their row's power of two in one instruction for two of them, exactly; V codes come through the 8-bit transpose read and
 //   become bf16 as they are, and their rows' powers go into the probabilities, exactly too.
 //   The waves' partial results are merged through LDS; where a head is in parts, the workgroup that finishes it last merges those, or, of many parts and query heads, a launch more does.
-// One token of one sequence, 8 KV heads of 128, 32 query heads, us: 300 keys e4m3 7.1 (an empty launch is 4.7), 519 bf16 8.8, 131072 bf16 97 (5.5 TB/s), e4m3 48; 64 query heads, four caches of
-// 16384, e4m3 27 (5.0 TB/s).
+// One token, 8 KV heads of 128, caches not on the chip, us: one sequence with 32 query heads, 300 keys e4m3 7.1 (an empty launch is 2.6), 519 bf16 8.7, 131072 bf16 96.7 (5.6 TB/s), e4m3 54.9 (4.9 TB/s);
+// 64 query heads, four e4m3 caches of 16384 31.1 (4.3 TB/s).  Of each some 10 us pass before the first rows arrive and while results are put together.
 // Pages.  A page holds a multiple of 16 positions, so that each half of a tile lies in one: lane l of a wave keeps the page of half l of its next 64, and a
 // tile's two are lane reads.  What lies behind the length in the last page is read with it, and left out by selects; a half in no page at all is read from page 0 and left out.
 #include "ls_device.h"
@@ -20,8 +20,8 @@
 namespace ls {
 
 constexpr int PG_WAVES = 8, PG_THREADS = 64 * PG_WAVES, PG_BATCH = 8;
-// Parts x query heads that the last workgroup of a head puts together itself; it reads their results alone, 30 to 50 KB a us.  Itself / by a launch more, us: 32 x 4 97.0 / 96.5, 8 x 8 26.7 / 28.0,
-// 17 x 8 10.8 / 12.3, 128 x 8 15.4 / 11.9, 128 x 32 53 / 13, 256 x 32 176 / 22.
+// Parts x query heads that the last workgroup of a head puts together itself; it reads their results alone, 30 to 50 KB a us.  Itself / by a launch more, us: 32 x 4 96.7 / 97.0, 8 x 8 31.1 / 32.9,
+// 17 x 8 12.2 / 13.4, 128 x 8 15.2 / 12.4, 128 x 32 48 / 13, 256 x 32 158 / 23.
 constexpr int PAGED_JOIN = 320;
 
 template <int D, bool E4M3>

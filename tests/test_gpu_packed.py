@@ -94,6 +94,15 @@ def test_items_beyond_what_is_resident():
     _check(q, k, v, keys, keys, out, lse, heads=[0, 13, 31])
 
 
+@pytest.mark.parametrize("Hkv,keys", [(4, [100] * 50 + [2500]), (4, [2500] + [100] * 50), (8, [100] * 50 + [1000, 1, 0, 800, 1250])])
+def test_one_long_sequence_among_short_ones(Hkv, keys):
+    """More items than workgroups are resident; one so long that the sequences are put in order, and none."""
+    q, k, v = _inputs(4, 4 * Hkv, Hkv, 128, keys, keys, torch.bfloat16)
+    print("packed one long", Hkv, len(keys), flush=True)
+    out, lse = _run(q, k, v, keys, keys)
+    _check(q, k, v, keys, keys, out, lse, heads=[0, 7, 15])
+
+
 @pytest.mark.parametrize("room", [0, 40 * (128 * 128 + 256) * 4])
 def test_less_workspace(room):
     """Without room for parts items are whole, with some there are fewer parts."""
