@@ -11,7 +11,7 @@
 //   become bf16 as they are, and their rows' powers go into the probabilities, exactly too.
 //   The waves' partial results are merged through LDS; where a head is in parts, the workgroup that finishes it last merges those, or, of many parts and query heads, a launch more does.
 // One token, 8 KV heads of 128, caches not on the chip, us: one sequence with 32 query heads, 300 keys e4m3 7.1 (an empty launch is 2.6), 519 bf16 8.7, 131072 bf16 96.7 (5.6 TB/s), e4m3 54.9 (4.9 TB/s);
-// 64 query heads, four e4m3 caches of 16384 31.1 (4.3 TB/s).  Of each some 10 us pass before the first rows arrive and while results are put together.
+// 64 query heads, four e4m3 caches of 16384 31.1 (4.3 TB/s).  About 5 us of each pass before the first rows arrive and while results are put together (135, 212 and 537 MB take that more than at 5.1, 4.1 and 5.8 TB/s).
 // Pages.  A page holds a multiple of 16 positions, so that each half of a tile lies in one: lane l of a wave keeps the page of half l of its next 64, and a
 // tile's two are lane reads.  What lies behind the length in the last page is read with it, and left out by selects; a half in no page at all is read from page 0 and left out.
 #include "ls_device.h"
