@@ -53,6 +53,7 @@ __device__ __forceinline__ uint32_t lanes_sum(uint32_t x) { return (uint32_t)__b
 struct PackedWork {
     PackedSeq seq;            // of sequence `lane` (of 64 at a time), or `index`
     int G, lane, index;
+    int q0, k0;               // first rows of sequence `lane` (of 64 at a time; not of `index`), packed
     // the item, its part, and the unit it is
     int s, block, part, length;
     bool stopped = false;     // a sequence before had starts that are none
@@ -60,9 +61,11 @@ struct PackedWork {
         const int i = s0 + lane;
         bool bad = false;
         seq = PackedSeq{0, 0};
+        q0 = k0 = 0;
         if (i < a.B) {
             if (a.q_starts) {
-                const int32_t q0 = a.q_starts[i], q1 = a.q_starts[i + 1], k0 = a.k_starts[i], k1 = a.k_starts[i + 1];
+                q0 = a.q_starts[i]; k0 = a.k_starts[i];
+                const int32_t q1 = a.q_starts[i + 1], k1 = a.k_starts[i + 1];
                 bad = !starts_ok(q0, q1, a.n_hat) || !starts_ok(k0, k1, a.n);
                 seq = PackedSeq{k1 - k0, q1 - q0};
             } else {
@@ -179,7 +182,8 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
     if (!(a.cut.units ? w.find_part(a, rank) : w.find_in_order(a, rank))) return;
     const int sl64 = uniform(w.s) & 63, s = a.sorted ? __builtin_amdgcn_readlane(w.index, sl64) : uniform(w.s), block = uniform(w.block);
     const int nk = __builtin_amdgcn_readlane(w.seq.keys, sl64), nq = __builtin_amdgcn_readlane(w.seq.queries, sl64);
-    const int64_t q0 = a.q_starts ? a.q_starts[s] : 0, k0 = a.k_starts ? a.k_starts[s] : 0, pad = a.q_starts ? 0 : s;
+    // (loaded again from the starts they would be waited for once more)
+    const int64_t q0 = __builtin_amdgcn_readlane(w.q0, s & 63), k0 = __builtin_amdgcn_readlane(w.k0, s & 63), pad = a.q_starts ? 0 : s;
     const int steps = packed_steps(PackedSeq{nk, nq}, G, block);
     const int length = uniform(w.length), h0 = uniform(w.part) * length, h1 = steps - h0 > length ? h0 + length : steps;         // steps of this part
     const bool cut = steps > length;
