@@ -14,6 +14,10 @@
 namespace ls {
 
 constexpr int MOVE_THREADS = 256;
+// The chip's last-level cache.  A call that moves more reads pages past it: they would only displace the rows that it writes, which are wanted next.  Rows read back, together with a call that reads those,
+// us: four caches of 16384 e4m3 246 -> 233, bf16 268 -> 249; of less data, which the next call may still find there, 16384 rows to fp32 94 for 87 where the same pages are read again.
+// Rows that a call writes, or reads from the caller's tensor, never pass it by: 32768 rows read back would take 32 instead of 42 us, and with a call that reads them 131 instead of 123.
+constexpr int64_t ON_CHIP = 256 << 20;
 
 // Largest over the LPR (8 or 16) neighbouring lanes of a row
 template <int LPR>
@@ -51,6 +55,13 @@ template <> struct Eight<float> {
     __device__ float at(int i) const { return v[i / 4][i % 4]; }
     __device__ void set(int i, float x) { v[i / 4][i % 4] = x; }
 };
+
+// Loads by f(load) of what is wanted once (`once`, wave-uniform) or again.  The empty statements keep the two sides apart: joined, all would be ordinary loads.
+template <typename F>
+__device__ __forceinline__ void load_by(bool once, F f) {
+    if (once) { asm volatile(""); f([](auto* p) { return __builtin_nontemporal_load(p); }); asm volatile(""); }
+    else f([](auto* p) { return *p; });
+}
 
 // grid (blocks of rows, groups of KV heads).  A workgroup has 256 / (d / 8) neighbouring rows, and of a row d / 8 lanes eight values each: whose sequence each
 // row is of, and the place that the table gives it, are found once for all its heads and for K and V.
@@ -139,11 +150,17 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) { Eight<T> x; x.load(rows[t] + h * step[t]); put(x, h, t); }
     } else {
-        auto get = [&](int h, int t, uint2& w, Eight<bf16_t>& x, uint32_t& E) {
+        auto get = [&](auto load, int h, int t, uint2& w, Eight<bf16_t>& x, uint32_t& E) {
             const int64_t r = place + ((int64_t)h << a.cache.page_log);
             const unsigned char* src = pool[t] + r * (D * DST) + 8 * part * DST;
-            if constexpr (E4M3) { w = *reinterpret_cast<const uint2*>(src); E = exps[t][r]; }
-            else x.load(src);
+            if constexpr (E4M3) {
+                typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+                const u32x2 y = load(reinterpret_cast<const u32x2*>(src));
+                w = make_uint2(y.x, y.y);
+                E = exps[t][r];
+            } else {
+                x.v = load(reinterpret_cast<const bf16x8*>(src));
+            }
         };
         auto give = [&](int h, int t, const uint2& w, const Eight<bf16_t>& x, uint32_t E) {
             Eight<T> y;
@@ -165,26 +182,29 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
         int h = h0;
         for (; h + 2 <= h1; h += 2) {
             uint2 w[4]; Eight<bf16_t> x[4]; uint32_t E[4];
+            load_by(a.once, [&](auto load) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) get(h + j / 2, j & 1, w[j], x[j], E[j]);
+            for (int j = 0; j < 4; ++j) get(load, h + j / 2, j & 1, w[j], x[j], E[j]);
+            });
 #pragma unroll
             for (int j = 0; j < 4; ++j) give(h + j / 2, j & 1, w[j], x[j], E[j]);
         }
         for (; h < h1; ++h)
 #pragma unroll
-            for (int t = 0; t < 2; ++t) { uint2 w; Eight<bf16_t> x; uint32_t E; get(h, t, w, x, E); give(h, t, w, x, E); }
+            for (int t = 0; t < 2; ++t) { uint2 w; Eight<bf16_t> x; uint32_t E; load_by(a.once, [&](auto load) { get(load, h, t, w, x, E); }); give(h, t, w, x, E); }
     }
 }
 
 template <bool WRITE, typename T, bool E4M3, int D>
 static hipError_t run_move_t(MoveArgs a, hipStream_t st) {
-    constexpr int ROWS = MOVE_THREADS / (D / 8);
+    constexpr int ROWS = MOVE_THREADS / (D / 8), BYTES = Elem<T>::bytes + (E4M3 ? 1 : 2);
     const int64_t rows = (a.starts ? 1 : (int64_t)a.B) * a.n_hat;
     const int64_t blocks = (rows + ROWS - 1) / ROWS;
     // All heads of a row in one workgroup where there are rows enough: what a row is and where it goes is found once for them.  Two heads of them otherwise, for more workgroups.  All heads / two, us:
     // four caches of 16384, packed 81 / 86, padded 81 / 79, 16384 rows of 32 heads of 64 49 / 51, four single rows 5.5 / 4.7, 3400 rows of fp32 5.8 / 5.4.
     a.heads = a.cache.Hkv;
     while (a.heads > 2 && blocks * ((a.cache.Hkv + a.heads - 1) / a.heads) < 2048) a.heads = (a.heads + 1) / 2;
+    a.once = rows * a.cache.Hkv * (2 * D * BYTES) > ON_CHIP;
     hipLaunchKernelGGL((move_kernel<WRITE, T, E4M3, D>), dim3((uint32_t)blocks, (a.cache.Hkv + a.heads - 1) / a.heads), dim3(MOVE_THREADS), 0, st, a);
     return hipGetLastError();
 }

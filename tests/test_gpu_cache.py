@@ -387,6 +387,44 @@ def test_powers_far_from_one():
     _check(p, q, table, [40], out, lse)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_more_than_the_chip_holds(kind):
+    """Calls on more than 256 MB, whose pages are read past the caches: attention over 73001 keys of 16 heads (the sequences' pages repeat), and rows of nine heads read back."""
+    rng = np.random.default_rng(18)
+    lens, H, d, page = [70000, 3001], 16, 128, 256
+    p = pu.pool(rng, 40, H, page, d, kind)
+    q = pu.rnd(rng, 2, H, d, scale=1.5)
+    table = torch.from_numpy(rng.integers(0, 40, (2, 274)).astype(np.int32))
+    assert sum(lens) * H * 2 * d * (2 if kind == "bf16" else 1) > 256 << 20
+    print("paged past the chip", kind, flush=True)
+    out, lse, status = _attend(p, q, table, lens, times=2)
+    assert status == 0
+    K, V = pu.stored(p, "k"), pu.stored(p, "v")
+    for b, n in enumerate(lens):
+        at = torch.arange(n)
+        pg, pl = table[b, at // page].long(), at % page
+        for h in (0, 9, 15):
+            pu.check(out[b, h:h + 1], lse[b, h:h + 1], pu.attention(q[b, h:h + 1], K[pg, h, pl], V[pg, h, pl], np.full(1, n), d ** -0.5), torch.bfloat16)
+
+    lens, H, n = [36000, 35977], 9, 36000
+    p = {name: x[:, :H].contiguous() for name, x in p.items()}
+    assert 2 * n * H * 2 * d * (4 if kind == "bf16" else 3) > 256 << 20
+    rows = [torch.full((2, H, n, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ctx = binding.Context(workspace=0)
+    print("read past the chip", kind, flush=True)
+    ctx.ls_cache_read(binding.make_shape(2, H, H, d, n, n, 1, "bf16"), _cache(p), table.cuda(), *rows, pos=_i32([5, 100]), count=_i32(lens))
+    torch.cuda.synchronize()
+    assert ctx.ls_poll_status() == 0
+    for name, got in zip(("k", "v"), rows):
+        held = pu.stored(p, name).to(torch.bfloat16).cuda()
+        for b, m in enumerate(lens):
+            at = torch.arange(m) + [5, 100][b]
+            pg, pl = table[b, at // page].long().cuda(), (at % page).cuda()
+            for h in range(H):
+                assert torch.equal(got[b, h, :m], held[pg, h, pl])
+            assert torch.isnan(got[b, :, m:]).all()
+
+
 def test_the_last_pages_of_a_large_pool():
     """Pages whose rows lie beyond 2^31 elements and 2^32 bytes of the pool."""
     pages, Hkv, page, d = 70000, 2, 128, 128
