@@ -6,7 +6,7 @@
 // fifteen binades of e4m3 below a row's largest value.
 //
 // Bound by memory: each row is read and written once, and of each position the table's entry.  8 KV heads of 128, e4m3, us: 32768 bf16 rows written 43 (4.7 TB/s, read and written), four caches of
-// 16384 read back 81 (5.0 TB/s; a copy of 1 GiB reaches 5.15); one row of each of four sequences written 4.6, where an empty launch is 2.6.
+// 16384 read back 79 (5.1 TB/s; a copy of 1 GiB reaches 5.15); one row of each of four sequences written 4.6, where an empty launch is 2.6.
 #include <type_traits>
 #include "ls_device.h"
 #include "ls_internal.h"
@@ -201,7 +201,7 @@ static hipError_t run_move_t(MoveArgs a, hipStream_t st) {
     const int64_t rows = (a.starts ? 1 : (int64_t)a.B) * a.n_hat;
     const int64_t blocks = (rows + ROWS - 1) / ROWS;
     // All heads of a row in one workgroup where there are rows enough: what a row is and where it goes is found once for them.  Two heads of them otherwise, for more workgroups.  All heads / two, us:
-    // four caches of 16384, packed 81 / 86, padded 81 / 79, 16384 rows of 32 heads of 64 49 / 51, four single rows 5.5 / 4.7, 3400 rows of fp32 5.8 / 5.4.
+    // four caches of 16384 (their pages through the caches), packed 81 / 86, padded 81 / 79, 16384 rows of 32 heads of 64 49 / 51, four single rows 5.5 / 4.7, 3400 rows of fp32 5.8 / 5.4.
     a.heads = a.cache.Hkv;
     while (a.heads > 2 && blocks * ((a.cache.Hkv + a.heads - 1) / a.heads) < 2048) a.heads = (a.heads + 1) / 2;
     a.once = rows * a.cache.Hkv * (2 * D * BYTES) > ON_CHIP;
