@@ -74,7 +74,8 @@ struct PackedWork {
         }
         const uint64_t none = __ballot(bad);
         if (stopped || (none != 0ull && lane >= __builtin_ctzll(none))) seq = PackedSeq{0, 0};
-        if (none != 0ull && !stopped && blockIdx.x == 0 && lane == 0) atomicOr(a.status, STAT_STARTS);
+        // Whoever comes upon them says so: one always does, since with starts a KV head has fewer items than workgroups (packed_items), and the ones without an item look at all sequences.
+        if (none != 0ull && !stopped && lane == 0) atomicOr(a.status, STAT_STARTS);
         stopped = stopped || none != 0ull;
     }
     __device__ int longer(int x) const { return (int)lanes_sum((uint32_t)packed_longer(seq, G, x)); }

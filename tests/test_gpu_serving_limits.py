@@ -1,0 +1,36 @@
+"""Calls on pages and packed sequences at the ends of what they allow: many sequences, many rows, infinities across parts, every exponent byte."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2507_13681_amd import binding
+from tests import paged_util as pu
+from tests.test_gpu_packed import _check, _inputs, _run, _starts
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(2, 1), (4, 2), (6, 3), (8, 8), (16, 16)])
+@pytest.mark.parametrize("at", [0, 63, 64, 100, 129])
+@pytest.mark.parametrize("which", ["both", "q", "k"])
+def test_starts_that_are_none_behind_many_sequences(Hq, Hkv, at, which):
+    """130 sequences, of which one's starts descend: it and all behind it are passed by, and the status word says so, wherever it stands."""
+    rng = np.random.default_rng(at + Hq)
+    lens = [int(x) for x in rng.choice([0, 1, 5, 33, 40], 130)]
+    lens[at] = max(lens[at], 1)
+    T = sum(lens)
+    q, k, v = _inputs(at, Hq, Hkv, 64, lens, lens, torch.bfloat16)
+    good = _starts(lens)
+    bad = good.clone()
+    bad[at + 1:] = bad[at] - 1                             # (of sequence 0: leaves the rows)
+    qs, ks = (bad if which != "k" else good).cuda(), (bad if which != "q" else good).cuda()
+    shape = binding.make_shape(130, Hq, Hkv, 64, T, T, 1, "bf16")
+    ctx = binding.Context(workspace=binding.packed_workspace_bytes(shape))
+    out, lse = torch.full_like(q, 5.0, device="cuda"), torch.full((Hq, T), 5.0, device="cuda")
+    print("packed bad starts", Hq, Hkv, at, which, flush=True)
+    ctx.ls_packed_prefill(shape, q.cuda(), k.cuda(), v.cuda(), qs, ks, out, lse)
+    status = ctx.ls_poll_status()
+    end = int(good[at])
+    assert (out[end:] == 5.0).all() and (lse[:, end:] == 5.0).all()
+    _check(q[:end], k[:end], v[:end], lens[:at], lens[:at], out[:end].cpu(), lse[:, :end].cpu())
+    assert status == binding.LS_STAT_STARTS
