@@ -585,7 +585,8 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedArgs a) {
             for (int k = 0; k < 4; ++k) acc[k] *= corr;
 #pragma unroll
             for (int e = 0; e < NB; ++e) {
-                const float wgt = e0 + e * SUBS < here && ml[e].x > -INFINITY ? fast_exp2(ml[e].x - M) : 0.f;
+                if (e0 + e * SUBS >= here) break;          // (part e0 once more: with a weight of 0 its infinities would become NaN)
+                const float wgt = ml[e].x > -INFINITY ? fast_exp2(ml[e].x - M) : 0.f;
                 L += ml[e].y * wgt;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) acc[k] += x[e][k] * wgt;

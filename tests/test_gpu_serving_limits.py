@@ -34,3 +34,35 @@ def test_starts_that_are_none_behind_many_sequences(Hq, Hkv, at, which):
     assert (out[end:] == 5.0).all() and (lse[:, end:] == 5.0).all()
     _check(q[:end], k[:end], v[:end], lens[:at], lens[:at], out[:end].cpu(), lse[:, :end].cpu())
     assert status == binding.LS_STAT_STARTS
+
+
+def _odd_columns(n, d):
+    """(key, column, value): infinities all over the keys, a column each; a NaN; both infinities in one column."""
+    at = [(int(i * (n - 1) / (d - 5)), i, float("inf") if i % 2 else -float("inf")) for i in range(d - 4)]
+    return at + [(n // 3, d - 4, float("nan")), (n // 5, d - 3, float("inf")), (n - 1 - n // 5, d - 3, -float("inf"))]
+
+
+def _same_with_odd(out, got, want):
+    """got: what `out` becomes where `want` is not finite; the same bits elsewhere."""
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    fine = torch.isfinite(want)
+    assert torch.equal(got[fine], out[fine]) and torch.equal(got[torch.isinf(want)].double(), want[torch.isinf(want)].double())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d,keys,rows", [(128, 4000, 20), (64, 4000, 20), (128, 2777, 40), (64, 300, 300)])
+def test_infinite_values_of_cut_items(d, keys, rows, dtype):
+    """Single infinities in V reach the rows that see them in whichever part of an item they are, as in a whole one."""
+    q, k, v = _inputs(31, 4, 2, d, [keys], [rows], dtype, scale=0.5)
+    print("packed odd parts", d, keys, rows, dtype, flush=True)
+    v2 = v.clone()
+    for r, c, x in _odd_columns(keys, d):
+        v2[r, 0, c] = x
+    for room in (None, 0):                                 # in parts, and whole
+        out, lse = _run(q, k, v, [keys], [rows], room=room)
+        got, got_lse = _run(q, k, v2, [keys], [rows], room=room)
+        want = out.double().clone()
+        for r, c, x in _odd_columns(keys, d):
+            want[max(0, r - (keys - rows)):, :2, c] += x
+        _same_with_odd(out, got, want)
+        assert torch.equal(lse, got_lse)
