@@ -459,8 +459,9 @@ __global__ __launch_bounds__(2 * D) void paged_join_kernel(PagedArgs a) {
         m = m_new; o0 *= corr; o1 *= corr; l *= corr;
 #pragma unroll
         for (int e = 0; e < PG_BATCH; ++e) {
-            const float wgt = s0 + e * SUBS < w.cuts && ml[e].x > -INFINITY ? fast_exp2((ml[e].x - m) * a.scale_log2e) : 0.f;
-            o0 += x[e].x * wgt; o1 += x[e].y * wgt; l += ml[e].y * wgt;
+            const bool is = s0 + e * SUBS < w.cuts;            // (behind them part s0 once more: its infinities times 0 would be NaN)
+            const float wgt = ml[e].x > -INFINITY ? fast_exp2((ml[e].x - m) * a.scale_log2e) : 0.f;
+            o0 += is ? x[e].x * wgt : 0.f; o1 += is ? x[e].y * wgt : 0.f; l += is ? ml[e].y * wgt : 0.f;
         }
     }
     red[sub][tid % LANES] = make_float2(o0, o1);

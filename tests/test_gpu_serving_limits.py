@@ -5,6 +5,7 @@ import torch
 
 from paper_2507_13681_amd import binding
 from tests import paged_util as pu
+from tests.test_gpu_cache import _attend, _i32
 from tests.test_gpu_packed import _check, _inputs, _run, _starts
 
 pytestmark = pytest.mark.gpu
@@ -66,3 +67,27 @@ def test_infinite_values_of_cut_items(d, keys, rows, dtype):
             want[max(0, r - (keys - rows)):, :2, c] += x
         _same_with_odd(out, got, want)
         assert torch.equal(lse, got_lse)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,d", [
+    ([70, 70], 8, 2, 128),                           # one workgroup a head
+    ([2000, 2000], 4, 2, 128),                       # parts, put together by the last of them
+    ([1900], 4, 2, 64),
+    ([5003], 32, 1, 64),                             # parts, put together by a launch of their own
+    ([5003], 32, 1, 128), ([20000], 17, 1, 128)])
+def test_infinite_values_of_pages(lens, Hq, Hkv, d):
+    """Single infinities in V, however many parts there are and whoever puts them together."""
+    print("paged odd values", lens, Hq, Hkv, d, flush=True)
+    rng = np.random.default_rng(19)
+    pages = sum(-(-n // 16) for n in lens)
+    p = pu.pool(rng, pages, Hkv, 16, d, "bf16")
+    q, table = pu.rnd(rng, len(lens), Hq, d, scale=0.5), pu.table_for(rng, lens, 16, pages)
+    out, lse, _ = _attend(p, q, table, lens)
+    want = out.double().clone()
+    for r, c, x in _odd_columns(lens[0], d):
+        p["v"][table[0, r // 16].long(), 0, r % 16, c] = x
+        want[0, :Hq // Hkv, c] += x
+    got, got_lse, status = _attend(p, q, table, lens, times=2)
+    assert status == 0
+    _same_with_odd(out, got, want)
+    assert torch.equal(lse, got_lse)
