@@ -18,6 +18,8 @@ constexpr int MOVE_THREADS = 256;
 // us: four caches of 16384 e4m3 246 -> 233, bf16 268 -> 249; of less data, which the next call may still find there, 16384 rows to fp32 94 for 87 where the same pages are read again.
 // Rows that a call writes, or reads from the caller's tensor, never pass it by: 32768 rows read back would take 32 instead of 42 us, and with a call that reads them 131 instead of 123.
 constexpr int64_t ON_CHIP = 256 << 20;
+// Workgroups of a launch.  A dimension of a grid has less than 2^32 threads: of one that has more, HIP runs what is left of the number modulo 2^32, and says nothing.
+constexpr int64_t MOVE_GROUPS = 1 << 23;
 
 // Largest over the LPR (8 or 16) neighbouring lanes of a row
 template <int LPR>
@@ -70,8 +72,8 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
     constexpr int LPR = D / 8, ROWS = MOVE_THREADS / LPR, SRC = Elem<T>::bytes, DST = E4M3 ? 1 : 2;
     __shared__ int seq_s[ROWS], stop_s;
     const int tid = threadIdx.x, slot = tid / LPR, part = tid % LPR;
-    const int64_t row0 = (int64_t)blockIdx.x * ROWS;
-    const bool first = blockIdx.x == 0 && blockIdx.y == 0;
+    const int64_t row0 = (a.group0 + blockIdx.x) * ROWS;
+    const bool first = row0 == 0 && blockIdx.y == 0;
     int b = -1, i = 0;
     int64_t at = row0 + slot;                              // the row, and that of the tensor it is
     if (a.starts) {
@@ -205,8 +207,13 @@ static hipError_t run_move_t(MoveArgs a, hipStream_t st) {
     a.heads = a.cache.Hkv;
     while (a.heads > 2 && blocks * ((a.cache.Hkv + a.heads - 1) / a.heads) < 2048) a.heads = (a.heads + 1) / 2;
     a.once = rows * a.cache.Hkv * (2 * D * BYTES) > ON_CHIP;
-    hipLaunchKernelGGL((move_kernel<WRITE, T, E4M3, D>), dim3((uint32_t)blocks, (a.cache.Hkv + a.heads - 1) / a.heads), dim3(MOVE_THREADS), 0, st, a);
-    return hipGetLastError();
+    for (a.group0 = 0; a.group0 < blocks; a.group0 += MOVE_GROUPS) {
+        const int64_t here = blocks - a.group0 < MOVE_GROUPS ? blocks - a.group0 : MOVE_GROUPS;
+        hipLaunchKernelGGL((move_kernel<WRITE, T, E4M3, D>), dim3((uint32_t)here, (a.cache.Hkv + a.heads - 1) / a.heads), dim3(MOVE_THREADS), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 template <bool WRITE, typename T>
 static hipError_t run_move_d(const MoveArgs& a, int type, int d, hipStream_t st) {

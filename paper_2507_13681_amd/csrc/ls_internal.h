@@ -199,6 +199,7 @@ struct MoveArgs {
     const int32_t *starts, *count, *pos;       // as ls_cache_write has them
     int B, n_hat;
     int heads;                // KV heads of a workgroup
+    int64_t group0;           // first group of rows of this launch
     bool once;                // pages that are read are not read again soon
     int32_t* status;
 };

@@ -91,3 +91,23 @@ def test_infinite_values_of_pages(lens, Hq, Hkv, d):
     assert status == 0
     _same_with_odd(out, got, want)
     assert torch.equal(lse, got_lse)
+
+
+@pytest.mark.parametrize("d,n", [(64, (1 << 29) + 5), (128, (1 << 28) + 5)])
+def test_more_rows_than_a_launch_has_threads_for(d, n):
+    """Rows whose places take more than 2^32 threads to find (the rows share one place in memory): the last five are written, packed and padded."""
+    rows = pu.rnd(np.random.default_rng(1), 1, 1, d).cuda()
+    pool = torch.zeros(1, 1, 16, d, dtype=torch.bfloat16, device="cuda")
+    ctx, table = binding.Context(workspace=0), _i32([[0]])
+    print("cache many rows", d, n, flush=True)
+    cache = binding.PagedCache(pool.clone(), pool.clone())
+    ctx.ls_cache_write(binding.make_shape(1, 1, 1, d, 1, n, 1, "bf16"), cache, rows.expand(n, 1, d), rows.expand(n, 1, d), table, starts=_i32([n - 5, n]))
+    assert ctx.ls_poll_status() == 0
+    for x in (cache.k, cache.v):
+        assert torch.equal(x[0, 0, :5], rows[0].expand(5, d)) and (x[0, 0, 5:] == 0).all()
+    cache = binding.PagedCache(pool.clone(), pool.clone())
+    padded = rows[None].expand(2, 1, n // 2, d)
+    ctx.ls_cache_write(binding.make_shape(2, 1, 1, d, 1, n // 2, 1, "bf16"), cache, padded, padded, _i32([[-1], [0]]), count=_i32([0, 3]))
+    assert ctx.ls_poll_status() == 0
+    for x in (cache.k, cache.v):
+        assert torch.equal(x[0, 0, :3], rows[0].expand(3, d)) and (x[0, 0, 3:] == 0).all()
