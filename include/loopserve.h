@@ -285,7 +285,8 @@ typedef struct {
  * (Sec. 2.2 with M[a][b] = 1 iff b <= p_a), for sequences of different lengths:
  *     out[a] = sum_b softmax_b(scale * <q_a, k_b>) v_b.
  *
- *   shape: B sequences, Hq, Hkv, d, dtype, scale.  n: rows of k and v, n_hat: rows of q and out.  w is ignored.
+ *   shape: B sequences, Hq, Hkv, d, dtype, scale.  n >= 1: rows of k and v, n_hat >= 1: rows of q and out.  w is ignored.  Blocks of 128 rows (a query of a query head is
+ *        a row), one more for each sequence where they are packed, are at most 2^24 - 8 of all KV heads, and neighbouring rows of k and of v begin less than 64 MiB apart.
  *   q_starts, k_starts [B+1] int32, device memory: rows q_starts[s] .. q_starts[s+1] - 1 are sequence s's queries, likewise its
  *        keys; n and n_hat count all sequences' rows then.  Both NULL: every sequence has n keys and n_hat queries.
  *   The queries are the last positions of their sequence: query i of m sees the keys up to (keys of the sequence) - m + i,

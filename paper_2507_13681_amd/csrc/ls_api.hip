@@ -755,6 +755,7 @@ Wrong check_packed(const ls_shape* s, const ls_rows* q, const ls_rows* k, const 
     const int64_t seqs = q_starts ? 1 : s->B;
     if ((w = check_rows(q, s->dtype, s->d, seqs, s->n_hat, s->Hq, false)).code || (w = check_rows(out, s->dtype, s->d, seqs, s->n_hat, s->Hq, true)).code ||
         (w = check_rows(k, s->dtype, s->d, seqs, s->n, s->Hkv, false)).code || (w = check_rows(v, s->dtype, s->d, seqs, s->n, s->Hkv, false)).code) return w;
+    if (ls::packed_items(s->B, s->n_hat, s->Hkv, s->Hq / s->Hkv, q_starts != nullptr) > ls::PACKED_MOST_ITEMS) return {LS_ESHAPE, "too many rows"};
     const int64_t reach = 32 * (s->dtype == LS_BF16 ? 2 : 4);                // (a step's rows are reached by 32-bit offsets)
     if (k->row > (1LL << 31) / reach - 1 || v->row > (1LL << 31) / reach - 1) return {LS_ESHAPE, "rows of k or v are too far apart"};
     return FINE;

@@ -281,6 +281,7 @@ __host__ __device__ inline float packed_work(const PackedSeq& s, int G) {
     const float blocks = (float)packed_blocks(s.queries, G), before = s.keys > s.queries ? (float)((s.keys - s.queries) / PACKED_KEYS) : 0.f;
     return blocks * (before + 4.f) + 0.5f * PACKED_ROWS / PACKED_KEYS * blocks * (blocks + 1.f) / (float)G;
 }
+constexpr int64_t PACKED_MOST_ITEMS = (1 << 24) - 8;   // (of a grid of 2^32 threads HIP runs what is left modulo 2^32, without an error)
 constexpr int PACKED_SORTED = 64;            // with more sequences items go by sequence, whole
 // How a call cuts its items.  Parts are no more than the workgroups that are resident, so that they run at once (fp32 at d = 128 twice as many: one and two rounds, us, 1024 positions 51.6 / 47.0,
 // 300 and 40 new rows behind 2700 and none 103.5 / 76.6).  Whole / cut, us: follow-ups of 1 to 200 rows on 2900 to 20000 keys 460 / 83, 61 new rows of 12347 216 / 37, fp32 1024 positions of 8 heads of 128 149 / 47.

@@ -653,7 +653,6 @@ static hipError_t run_packed_t(PackedArgs a, hipStream_t st) {
     // the ranks of a KV head's items, rounded up to what the XCDs share
     int64_t groups = a.cut.units ? a.cut.units : (items + 7) / 8 * 8;
     if (!a.cut.units && 8 % a.Hkv != 0 && a.Hkv % 8 != 0) groups = items;
-    if (groups > 0x7FFFFFFF) return hipErrorInvalidValue;
     hipLaunchKernelGGL((packed_kernel<T, D>), dim3((uint32_t)groups), dim3(PK_THREADS), (PackCfg<T, D>::LDS), st, a);
     if (a.cut.units) hipLaunchKernelGGL((packed_join_kernel<T, D>), dim3((uint32_t)std::min<int64_t>(items * 4 * PackCfg<T, D>::DBLK, PK_JOIN_GROUPS)), dim3(256), 0, st, a);
     return hipGetLastError();

@@ -31,3 +31,18 @@ def test_packed_calls_have_workgroups_without_an_item(lib):
             lib.ls_debug_packed_counts(r, r, G, 0, 0, out)
             items += out[0]
         assert units[1] % Hkv == 0 and items < units[1] // Hkv
+
+
+HERE = 1 << 20                                             # an address, 16-byte aligned, that nothing follows
+
+
+@pytest.mark.parametrize("B,H,rows,starts,want", [
+    (1, 128, 1 << 24, True, -2), (1, 128, (1 << 24) - 256, True, 0),          # blocks of 128 rows of all heads, and one for each sequence and head
+    (128, 1, 1 << 24, False, -2), (128, 1, (1 << 24) - 128, False, 0), (4, 1, (1 << 29) - 512, False, 0), (4, 1, 1 << 29, False, -2)])
+def test_more_blocks_than_a_launch_has_threads_for(lib, B, H, rows, starts, want):
+    """A call whose grid would have 2^32 threads is refused: HIP would run what is left of them."""
+    s = binding.make_shape(B, H, H, 64, 100, rows, 1, "bf16")
+    many = binding.LsRows(HERE, 0 if starts else rows * H * 64, H * 64, 64)
+    keys = binding.LsRows(HERE, 0 if starts else 100 * H * 64, H * 64, 64)
+    at = HERE if starts else None
+    assert lib.ls_debug_check_packed(C.byref(s), C.byref(many), C.byref(keys), C.byref(keys), at, at, C.byref(many), None) == want
