@@ -49,7 +49,10 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t lo, uint32_t hi, float f) {  
                                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true)}};
     return __builtin_bit_cast(bf16x8, u);
 }
-__device__ __forceinline__ float power_of_byte(uint32_t w, int i) { return __builtin_bit_cast(float, (w >> (8 * i) & 0xFFu) << 23); }
+// Byte i of w as the scale of a conversion, which looks at the exponent alone (0: 2^-127, 255: the result is NaN), ..
+__device__ __forceinline__ float scale_of_byte(uint32_t w, int i) { return __builtin_bit_cast(float, (w >> (8 * i) & 0xFFu) << 23); }
+// .. and as a number, which that of the code of one is (0 and 255 as bits of a float would be zero and infinity)
+__device__ __forceinline__ float power_of_byte(uint32_t w, int i) { return __builtin_amdgcn_cvt_scalef32_f32_fp8(0x38, scale_of_byte(w, i), 0); }
 
 __device__ __forceinline__ int paged_tiles(int n) { return (int)(((uint32_t)n + PAGED_TILE - 1) / PAGED_TILE); }
 
@@ -246,7 +249,7 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
                 bf16x8 kf;
                 if constexpr (E4M3) {
                     const uint4 w = __builtin_bit_cast(uint4, kr[e][c / 2]);
-                    kf = c % 2 ? bf16_of(w.z, w.w, power_of_byte(kx[e], 0)) : bf16_of(w.x, w.y, power_of_byte(kx[e], 0));
+                    kf = c % 2 ? bf16_of(w.z, w.w, scale_of_byte(kx[e], 0)) : bf16_of(w.x, w.y, scale_of_byte(kx[e], 0));
                 } else {
                     kf = __builtin_bit_cast(bf16x8, kr[e][c]);
                 }
@@ -292,7 +295,7 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
             }
             if constexpr (E4M3) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) x[r] = whole || x[r] > 0.f ? x[r] * vp[r] : 0.f;        // (behind the length the bytes may be anything)
+                for (int r = 0; r < 8; ++r) x[r] = whole || (16 * (r >> 2) + 4 * q + (r & 3) < left && hf[r >> 2].on) ? x[r] * vp[r] : 0.f;        // (behind the length the bytes may be anything)
             }
             Frag<T> f;
             pack_frag(f, x);                                           // contraction index 8 q + r <-> key 16 (r / 4) + 4 q + r % 4

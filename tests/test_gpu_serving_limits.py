@@ -111,3 +111,72 @@ def test_more_rows_than_a_launch_has_threads_for(d, n):
     assert ctx.ls_poll_status() == 0
     for x in (cache.k, cache.v):
         assert torch.equal(x[0, 0, :3], rows[0].expand(3, d)) and (x[0, 0, 3:] == 0).all()
+
+
+def _every_byte(part):
+    """64 codes, a row of them for each exponent byte, and the values that they stand for."""
+    codes = (torch.arange(64) + 64 * part).to(torch.uint8)
+    value = codes.view(pu.E4M3).double()[None] * torch.exp2(torch.arange(256).double() - 127)[:, None]
+    value[255] = float("nan")
+    return codes, value
+
+
+def _equal(got, want):
+    return ((got == want) | (torch.isnan(got) & torch.isnan(want))).all(-1)
+
+
+@pytest.mark.parametrize("part", [0, 1, 2, 3])
+def test_every_exponent_byte_is_attended_to(part):
+    """One key a sequence, whose output is its row of V; with an equal row at the byte 0 or 255 behind the length, which does not matter."""
+    codes, value = _every_byte(part)
+    v = codes.expand(256, 1, 16, 64).contiguous()
+    E = torch.arange(256).to(torch.uint8)[:, None, None].expand(256, 1, 16).contiguous()
+    E[:, :, 1] = 255
+    p = dict(k=torch.full((256, 1, 16, 64), 0x38, dtype=torch.uint8), v=v, k_exp=torch.full((256, 1, 16), 127, dtype=torch.uint8), v_exp=E)
+    print("paged bytes of V", part, flush=True)
+    out, _, status = _attend(p, torch.ones(256, 1, 64).bfloat16(), torch.arange(256, dtype=torch.int32)[:, None], [1] * 256)
+    assert status == 0
+    same = _equal(out[:, 0], value.to(torch.bfloat16))
+    assert same.all(), torch.nonzero(~same)[:, 0].tolist()
+
+
+def test_every_exponent_byte_of_keys():
+    """Logits of single keys: a query that is a power of two in one column brings the stored value, as bf16 has it, near one; the normaliser of one key is its logit."""
+    codes, value = _every_byte(0)
+    bits = torch.arange(256)
+    E = bits.to(torch.uint8)[:, None, None].expand(256, 1, 16).contiguous()
+    p = dict(k=codes.expand(256, 1, 16, 64).contiguous(), v=torch.full((256, 1, 16, 64), 0x38, dtype=torch.uint8), k_exp=E, v_exp=torch.full((256, 1, 16), 127, dtype=torch.uint8))
+    back = torch.exp2((127 - bits).clamp_min(-126).double())
+    for col in (1, 3, 8, 9, 40, 63):
+        q = torch.zeros(256, 1, 64, dtype=torch.bfloat16)
+        q[:, 0, col] = back.to(torch.bfloat16)
+        print("paged bytes of K", col, flush=True)
+        out, lse, _ = _attend(p, q, bits.int()[:, None], [1] * 256, scale=1.0)
+        x, got = value.to(torch.bfloat16).double()[:, col] * back, lse[:, 0].double()
+        nan = torch.isnan(x)
+        # the factor log2(e), the product with it, the factor ln(2) and the product with that: 2^-24 each
+        assert torch.equal(torch.isnan(got), nan) and ((got - x).abs() <= 2.0 ** -22 * x.abs())[~nan].all(), col
+        assert (out[~nan] == 1.0).all() and torch.isnan(out[nan]).all()
+
+
+@pytest.mark.parametrize("n,at", [(2, 1), (40, 35), (40, 3), (64, 50)])
+@pytest.mark.parametrize("how", ["byte", "code", "bf16"])
+def test_a_value_that_is_none_and_weighs_nothing(how, n, at):
+    """A key that is seen with a weight of 0 in fp32, and whose row of V is no number, in whole and partial tiles: 0 times NaN."""
+    rng = np.random.default_rng(44)
+    kind = "bf16" if how == "bf16" else "e4m3"
+    p = pu.pool(rng, 4, 1, 16, 64, kind)
+    k = torch.zeros(4, 1, 16, 64)
+    k[..., 0] = 1.0
+    k[at // 16, 0, at % 16, 0] = -8.0
+    if kind == "bf16":
+        p["k"], p["v"][at // 16, 0, at % 16] = k.bfloat16(), float("nan")
+    else:
+        p["k_exp"] = pu.exponents(k)
+        p["k"] = pu.codes(k, p["k_exp"])
+        p["v_exp" if how == "byte" else "v"][at // 16, 0, at % 16] = 255 if how == "byte" else 0x7F
+    q = torch.zeros(1, 2, 64).bfloat16()
+    q[..., 0] = 100.0
+    print("paged weightless", how, n, at, flush=True)
+    out, lse, status = _attend(p, q, torch.arange(4, dtype=torch.int32)[None], [n], scale=1.0)
+    assert status == 0 and torch.isnan(out).all() and torch.isfinite(lse).all()
