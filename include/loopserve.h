@@ -267,7 +267,9 @@ typedef enum { LS_CACHE_BF16 = 0, LS_CACHE_E4M3 = 1 } ls_cache_type;
 /* A pool of pages.  Page p holds `page` neighbouring positions of one sequence, of all KV heads: k, v [pages,Hkv,page,d],
  * contiguous, 16-byte aligned.  LS_CACHE_BF16: bf16.  LS_CACHE_E4M3: 8-bit floats (1 sign, 4 exponent, 3 fraction bits, bias 7, no
  * infinities, 0x7F and 0xFF are NaN) and, in k_exp, v_exp [pages,Hkv,page], a byte E for each row: a stored value stands
- * for code * 2^(E - 127), which bf16 and fp32 hold exactly (but for 2^128, to which magnitudes from 1.9375 * 2^127 on round: infinity).
+ * for code * 2^(E - 127), and for NaN where E is 255.  ls_cache_write makes E from 10 to 247, of which bf16 and fp32 hold every value exactly (but for
+ * 2^128, to which magnitudes from 1.9375 * 2^127 on round: infinity).  Pages that a caller fills may have other bytes: ls_cache_read rounds their values to
+ * the rows' type, ls_paged_attend rounds those of K to bf16.  A softmax weight times the power 2^(E - 127) of its row of V is a bf16 there, which has fewer bits below 2^-126.
  * Where a sequence's pages are is a row of `table` [B,max_pages] int32, device memory: positions p * page .. of sequence b lie in
  * page table[b][p].  Several sequences may share pages that are read.  A page number outside [0, pages), and a position beyond max_pages * page, is nowhere:
  * rows of it are neither written nor read, keys of it are not seen, and LS_STAT_PAGE_RANGE is set. */

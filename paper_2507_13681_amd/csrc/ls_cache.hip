@@ -167,13 +167,19 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
         auto give = [&](int h, int t, const uint2& w, const Eight<bf16_t>& x, uint32_t E) {
             Eight<T> y;
             if constexpr (E4M3) {
-                const float f = power_of(E);
+                const float f = power_of(E);               // (of which a conversion looks at the exponent alone: 2^-127 for 0, and NaN comes of 255)
                 const uint32_t u[2] = {w.x, w.y};
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-                    const bf16x2 z = (e & 2) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[e / 4], f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[e / 4], f, false);
-                    y.set(e, (float)z.x); y.set(e + 1, (float)z.y);
+                    if constexpr (std::is_same<T, float>::value) {               // (by way of bf16 codes of the bytes 0 to 2 would lose bits)
+                        typedef __attribute__((ext_vector_type(2))) float f32x2;
+                        const f32x2 z = (e & 2) ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(u[e / 4], f, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(u[e / 4], f, false);
+                        y.set(e, z.x); y.set(e + 1, z.y);
+                    } else {
+                        typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+                        const bf16x2 z = (e & 2) ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[e / 4], f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u[e / 4], f, false);
+                        y.set(e, (float)z.x); y.set(e + 1, (float)z.y);
+                    }
                 }
             } else {
 #pragma unroll

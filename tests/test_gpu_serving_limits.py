@@ -125,6 +125,23 @@ def _equal(got, want):
     return ((got == want) | (torch.isnan(got) & torch.isnan(want))).all(-1)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("part", [0, 1, 2, 3])
+def test_every_exponent_byte_is_read(part, dtype):
+    """code * 2^(E - 127), rounded to the rows' type; 255: no number."""
+    codes, value = _every_byte(part)
+    k = codes.expand(16, 1, 16, 64).contiguous().cuda()
+    E = torch.arange(256).to(torch.uint8).view(16, 1, 16).cuda()
+    rows = [torch.zeros(256, 1, 64, dtype=dtype, device="cuda") for _ in range(2)]
+    print("cache bytes", part, dtype, flush=True)
+    binding.Context(workspace=0).ls_cache_read(binding.make_shape(1, 1, 1, 64, 1, 256, 1, dtype), binding.PagedCache(k, k.clone(), E, E.clone()),
+                                               torch.arange(16, dtype=torch.int32, device="cuda")[None], *rows, starts=_i32([0, 256]))
+    torch.cuda.synchronize()
+    for x in rows:
+        same = _equal(x[:, 0].cpu(), value.to(dtype))
+        assert same.all(), torch.nonzero(~same)[:, 0].tolist()
+
+
 @pytest.mark.parametrize("part", [0, 1, 2, 3])
 def test_every_exponent_byte_is_attended_to(part):
     """One key a sequence, whose output is its row of V; with an equal row at the byte 0 or 255 behind the length, which does not matter."""
