@@ -9,6 +9,7 @@ otherwise -- there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import os
 
@@ -142,12 +143,21 @@ def load_library():
 
 
 def _load_native():
-    """The CPython modules over the C ABI, built beside the library."""
+    """The CPython module over the C ABI, built beside the library."""
     try:
-        from . import _lsnative, _lspages
+        from . import _lsnative
     except ImportError as e:
-        raise LoopServeError(f"_lsnative.so or _lspages.so cannot be loaded ({e}): build them with `python -m paper_2507_13681_amd.build`") from e
-    return _lsnative, _lspages
+        raise LoopServeError(f"_lsnative.so cannot be loaded ({e}): build it with `python -m paper_2507_13681_amd.build`") from e
+    return _lsnative
+
+
+def _load_pages():
+    """The module of the calls on pages and packed sequences, which reads tensors as the PyTorch that it was built against lays them out, and refuses another."""
+    try:
+        from . import _lspages
+    except ImportError as e:
+        raise LoopServeError(f"_lspages.so cannot be loaded ({e}): build it with `python -m paper_2507_13681_amd.build`") from e
+    return _lspages
 
 
 def make_shape(B, Hq, Hkv, d, n, n_hat, w, dtype, scale=0.0) -> LsShape:
@@ -211,7 +221,7 @@ class Context:
 
     def __init__(self, shape: LsShape | None = None, budget: int = 0, device: int = 0, workspace: int | None = None):
         self.lib = load_library()
-        self.native, self.pages = _load_native()
+        self.native = _load_native()
         if workspace is None:
             workspace = workspace_bytes(shape, budget)
             if workspace == 0:
@@ -284,6 +294,11 @@ class Context:
         rc = self.native.decode_attend(self.hv, shape, q, k_c, v_c, cnt, k_t, v_t, out, lse)
         if rc:
             self._check(rc)
+
+    @functools.cached_property
+    def pages(self):
+        """Loaded by the first call that needs it: the others do without."""
+        return _load_pages()
 
     # -- pages and packed sequences.  Rows are [rows, heads, d] where starts say whose they are, [B, heads, rows, d] otherwise, of any strides but
     # the last; the native marshalling checks types, sizes and devices, since the library sees addresses only (ValueError)

@@ -52,9 +52,10 @@ def build_native() -> str:
     import torch
     at = os.path.dirname(torch.__file__)
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-Wall", "-std=c++17", "-shared", "-fPIC", "-DUSE_ROCM", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}",
+           f'-DLS_TORCH="{torch.__version__}"',
            "-isystem", at + "/include", "-isystem", at + "/include/torch/csrc/api/include", "-I" + sysconfig.get_path("include"),
            os.path.join(CSRC, "ls_pages.cpp"), "-o", PAGES, "-L" + _DIR, "-l:libloopserve.so", "-Wl,-rpath,$ORIGIN",
-           "-L" + at + "/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath," + at + "/lib"]
+           "-L" + at + "/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"]                    # (those that the process has loaded, wherever they are)
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:
         raise RuntimeError("native module failed:\n" + r.stdout)

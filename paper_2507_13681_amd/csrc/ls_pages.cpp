@@ -160,6 +160,18 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lspages", nullptr, -1, methods, n
 }  // namespace
 
 PyMODINIT_FUNC PyInit__lspages() {
+    // Tensors are read by functions that the compiler took from PyTorch's headers: of another PyTorch they would read other places.
+    PyObject* torch = PyImport_ImportModule("torch");
+    PyObject* version = torch ? PyObject_GetAttrString(torch, "__version__") : nullptr;
+    Py_XDECREF(torch);
+    if (!version) return nullptr;
+    PyObject* text = PyObject_Str(version);
+    Py_DECREF(version);
+    if (!text) return nullptr;
+    const bool same = PyUnicode_CompareWithASCIIString(text, LS_TORCH) == 0;
+    if (!same) PyErr_Format(PyExc_ImportError, "built against PyTorch %s, and this is %U", LS_TORCH, text);
+    Py_DECREF(text);
+    if (!same) return nullptr;
     PyObject* c = PyImport_ImportModule("torch._C");
     if (!c) return nullptr;
     get_raw_stream = PyObject_GetAttrString(c, "_cuda_getCurrentRawStream");

@@ -1,8 +1,11 @@
 """Calls on pages and packed sequences at the ends of what they allow: many sequences, many rows, infinities across parts, every exponent byte."""
+import sys
+
 import numpy as np
 import pytest
 import torch
 
+import paper_2507_13681_amd as package
 from paper_2507_13681_amd import binding
 from tests import paged_util as pu
 from tests.test_gpu_cache import _attend, _i32
@@ -197,3 +200,25 @@ def test_a_value_that_is_none_and_weighs_nothing(how, n, at):
     print("paged weightless", how, n, at, flush=True)
     out, lse, status = _attend(p, q, torch.arange(4, dtype=torch.int32)[None], [n], scale=1.0)
     assert status == 0 and torch.isnan(out).all() and torch.isfinite(lse).all()
+
+
+def test_a_context_without_the_module_of_pages(monkeypatch):
+    """It is loaded by the first call on pages or packed sequences, and no other call needs it."""
+    monkeypatch.delitem(sys.modules, "paper_2507_13681_amd._lspages", raising=False)
+    monkeypatch.delattr(package, "_lspages", raising=False)
+    monkeypatch.setitem(sys.modules, "paper_2507_13681_amd._lspages", None)
+    rng = np.random.default_rng(45)
+    q, k = pu.rnd(rng, 1, 2, 1, 64).cuda(), pu.rnd(rng, 1, 1, 5, 64).cuda()
+    shape = binding.make_shape(1, 2, 1, 64, 5, 1, 1, "bf16")
+    print("context without pages", flush=True)
+    ctx = binding.Context(workspace=1 << 20)
+    out = torch.full_like(q[:, :, 0], float("nan"))
+    ctx.ls_decode_attend(shape, q[:, :, 0].contiguous(), k, k, None, None, None, out)
+    assert ctx.ls_poll_status() == 0 and torch.isfinite(out).all()
+    with pytest.raises(binding.LoopServeError, match="_lspages"):
+        ctx.ls_packed_prefill(shape, q, k, k, None, None, torch.empty_like(q))
+    monkeypatch.undo()
+    whole = torch.full_like(q, float("nan"))
+    ctx.ls_packed_prefill(shape, q, k, k, None, None, whole)
+    torch.cuda.synchronize()
+    assert torch.isfinite(whole).all()

@@ -2,6 +2,9 @@
 import ctypes as C
 import os
 import random
+import subprocess
+import sys
+import textwrap
 
 import pytest
 
@@ -46,3 +49,44 @@ def test_more_blocks_than_a_launch_has_threads_for(lib, B, H, rows, starts, want
     keys = binding.LsRows(HERE, 0 if starts else 100 * H * 64, H * 64, 64)
     at = HERE if starts else None
     assert lib.ls_debug_check_packed(C.byref(s), C.byref(many), C.byref(keys), C.byref(keys), at, at, C.byref(many), None) == want
+
+
+def _python(code):
+    return subprocess.run([sys.executable, "-c", textwrap.dedent(code)], cwd=os.path.dirname(build._DIR), stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+
+
+def test_the_calls_that_were_there_do_without_the_module_of_pages(lib):
+    r = _python("""
+        import sys
+        from paper_2507_13681_amd import binding
+        binding.load_library(), binding._load_native()
+        assert "paper_2507_13681_amd._lspages" not in sys.modules
+        sys.modules["paper_2507_13681_amd._lspages"] = None          # none that could be loaded
+        binding._load_native()
+        try:
+            binding._load_pages()
+        except binding.LoopServeError as e:
+            assert "_lspages" in str(e)
+        else:
+            raise AssertionError
+    """)
+    assert r.returncode == 0, r.stdout
+
+
+def test_another_pytorch_is_refused(lib):
+    """The module reads tensors by what the headers said of them."""
+    r = _python("""
+        import torch
+        from paper_2507_13681_amd import binding
+        was = str(torch.__version__)
+        torch.__version__ = "0.1"
+        try:
+            binding._load_pages()
+        except binding.LoopServeError as e:
+            assert was in str(e) and "0.1" in str(e), e
+        else:
+            raise AssertionError
+        torch.__version__ = was
+        assert binding._load_pages().packed_prefill
+    """)
+    assert r.returncode == 0, r.stdout
