@@ -222,3 +222,32 @@ def test_a_context_without_the_module_of_pages(monkeypatch):
     ctx.ls_packed_prefill(shape, q, k, k, None, None, whole)
     torch.cuda.synchronize()
     assert torch.isfinite(whole).all()
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_logits_as_large_as_the_header_allows(sign, dtype):
+    """Up to 2^30 in magnitude, 2^24 apart: each row is the value of the largest key that it sees, by its weight as the type has it, and its normaliser that key's logit."""
+    n, d = 64, 64
+    rng = np.random.default_rng(46)
+    order = torch.from_numpy(rng.permutation(n))
+    q, k, v = torch.zeros(n, 2, d), torch.zeros(n, 1, d), pu.rnd(rng, n, 1, d, dtype=dtype)
+    q[..., 0], k[:, 0, 0] = 2.0 ** 15, (order + 1).float() * 2.0 ** 9 * sign
+    q, k = q.to(dtype), k.to(dtype)
+    print("packed largest logits", sign, dtype, flush=True)
+    out, lse = _run(q, k, v, [n], [n], scale=1.0)
+    step = pu.HALF[dtype]
+    x = (k[:, 0, 0].double() * 2.0 ** 15)
+    for i in range(n):
+        best = int(x[:i + 1].argmax())
+        want = v[best, 0].double()
+        # the weight and the result are rounded once each in bf16; in fp32 the division and the product
+        assert ((out[i].double() - want).abs() <= 2.02 * step * want.abs()).all()
+        assert ((lse[:, i].double() - x[best]).abs() <= 2.0 ** -22 * x[best].abs()).all()
+    if dtype == torch.float32:
+        return
+    p = dict(k=k.view(4, 1, 16, d).contiguous(), v=v.view(4, 1, 16, d).contiguous())
+    out, lse, _ = _attend(p, q[:1], torch.arange(4, dtype=torch.int32)[None], [n], scale=1.0)
+    best = int(x.argmax())
+    assert ((out[0].double() - v[best, 0].double()).abs() <= 2.02 * step * v[best, 0].double().abs()).all()
+    assert ((lse[0].double() - x[best]).abs() <= 2.0 ** -22 * x[best].abs()).all()
