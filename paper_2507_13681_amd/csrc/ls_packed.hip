@@ -10,7 +10,8 @@
 // taken with the reference as it stands, and where a lane's sum exceeds a limit the step's softmax is done again with its maximum as the reference.
 // One sequence of 32768, 32 query and 8 KV heads of 128, bf16: 7.2 to 7.6 ms by card (1.16 to 1.22 PFLOP/s; a library product of 16384^3 reaches 1.33); 32 of 700 188 us; fp32, 4 query heads of 64, 1024, 300 and 37: 22 us.
 // Three workgroups a CU at d = 128.  With queries of zeros, the same work, it takes 5.6 ms, and with the softmax left out 6.5: the clock under load counts for more than any one pipeline.
-// What a row does not see weighs nothing, whatever it holds, and a row's reference moves for that row alone: its result has the same bits whatever its neighbours are.
+// What a row does not see weighs nothing, whatever it holds, and a row's reference moves for that row alone: of an item that is not cut its result has the same bits whatever its neighbours are.
+// (How long parts are, and so the order of the sums of a row in parts, follows from the work of the whole call.)
 // Items.  Which item a workgroup has follows from the starts, which only the device knows: a wave's lanes keep a sequence each and add up their blocks, those of the longest
 // sequences first where one is long beside the rest, the last block of each first; no launch ahead of this one puts them in order.
 #include <algorithm>
@@ -425,15 +426,16 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
             for (int i = 0; i < C::DBLK; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) oacc[i][r] *= corr;
-            sum = 0.f;
+            sum0 = 0.f; sum1 = 0.f;                        // (added up in the same order, for the lanes whose reference stays)
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int r = 0; r < 16; r += 2) {
                 const float e0 = fast_exp2(__builtin_fmaf(x[r], sc2, safe)), e1 = fast_exp2(__builtin_fmaf(x[r + 1], sc2, safe));
-                sum += e0; sum += e1;
+                sum0 += e0; sum1 += e1;
                 pr.set(r, e0, e1);
                 if (r % 4 == 2) __builtin_amdgcn_sched_barrier(0);
             }
+            sum = sum0 + sum1;
         }
         l_run += sum;
         __builtin_amdgcn_sched_barrier(0);

@@ -251,3 +251,19 @@ def test_logits_as_large_as_the_header_allows(sign, dtype):
     best = int(x.argmax())
     assert ((out[0].double() - v[best, 0].double()).abs() <= 2.02 * step * v[best, 0].double().abs()).all()
     assert ((lse[0].double() - x[best]).abs() <= 2.0 ** -22 * x[best].abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("Hq,Hkv,d", [(4, 4, 64), (4, 4, 128), (8, 2, 128)])
+def test_a_row_does_not_depend_on_its_neighbours_logits(Hq, Hkv, d, dtype):
+    """One row whose logits rise from step to step, so that its reference moves all the time: all others have the same bits as without that."""
+    n, at = 300, 159
+    q, k, v = _inputs(47, Hq, Hkv, d, [n], [n], dtype, scale=0.6)
+    q[..., 1], k[..., 1] = 0.0, (torch.arange(n) // 32).to(dtype)[:, None]
+    print("packed neighbour", Hq, Hkv, d, dtype, flush=True)
+    out, lse = _run(q, k, v, [n], [n], room=0)
+    q[at, :, 1] = 8.0 * d ** 0.5
+    got, got_lse = _run(q, k, v, [n], [n], room=0)
+    others = torch.arange(n) != at
+    assert torch.equal(got_lse[:, others], lse[:, others]) and torch.equal(got[others], out[others])
+    assert not torch.equal(got[at], out[at])
