@@ -300,6 +300,8 @@ typedef struct {
  *   out in dtype; a row that sees no key is all zeros, and one that sees a NaN logit is NaN, with its lse.  Rows of no sequence stay as they are.
  *   lse fp32 or NULL, [Hq,n_hat] (packed) or [B,Hq,n_hat]: natural log of the softmax denominator (-inf without a key)
  * Workspace: ls_packed_workspace_bytes (0 for an invalid shape); less is enough where the rows fill the chip, and slower elsewhere.
+ * Few rows on many keys are fast for up to 64 sequences, whose keys are then shared out among workgroups; of more, each workgroup has whole blocks of rows, and the call takes as long
+ * as the longest of them.
  */
 int ls_packed_prefill(ls_ctx* ctx, const ls_shape* shape, const ls_rows* q, const ls_rows* k, const ls_rows* v,
                       const int32_t* q_starts, const int32_t* k_starts, const ls_rows* out, float* lse, void* hip_stream);

@@ -14,7 +14,7 @@
 namespace ls {
 
 constexpr int MOVE_THREADS = 256;
-// The chip's last-level cache.  A call that moves more reads pages past it: they would only displace the rows that it writes, which are wanted next.  Rows read back, together with a call that reads those,
+// The chip's last-level cache.  A call whose tensors have more (all their rows: what `count` leaves of them only the device knows) reads pages past it: they would only displace the rows that it writes, which are wanted next.  Rows read back, together with a call that reads those,
 // us: four caches of 16384 e4m3 246 -> 233, bf16 268 -> 249; of less data, which the next call may still find there, 16384 rows to fp32 94 for 87 where the same pages are read again.
 // Rows that a call writes, or reads from the caller's tensor, never pass it by: 32768 rows read back would take 32 instead of 42 us, and with a call that reads them 131 instead of 123.
 constexpr int64_t ON_CHIP = 256 << 20;

@@ -217,7 +217,8 @@ __host__ __device__ inline bool paged_at_once(int64_t heads) { return heads * 4 
 constexpr int PAGED_WHOLE = 16;
 constexpr int PAGED_SHORTEST = 4, PAGED_SHORTEST_MANY = 32;                          // tiles of a part at least; of that many heads
 __host__ __device__ inline int paged_cuts(int tiles, int length) { return tiles <= PAGED_WHOLE ? 1 : (int)(((uint32_t)tiles + (uint32_t)length - 1) / (uint32_t)length); }
-// Tiles of a part of a call, of so many tiles in all: what `length` makes of them is counted until it is accepted
+// Tiles of a part of a call, of so many tiles in all: what `length` makes of them is counted until it is accepted, four times at most, and then `enough` is taken.  (24 ragged caches of 3212 tiles: 51, 57, 60
+// and 63 tiles are too many parts, 65 would do, 81 are taken.)
 struct PagedLength {
     int length, enough, slots, tries;        // enough: it will do, whatever the sequences are
     bool sorts;                              // not all parts run at once: the longest first
@@ -282,7 +283,9 @@ __host__ __device__ inline float packed_work(const PackedSeq& s, int G) {
     return blocks * (before + 4.f) + 0.5f * PACKED_ROWS / PACKED_KEYS * blocks * (blocks + 1.f) / (float)G;
 }
 constexpr int64_t PACKED_MOST_ITEMS = (1 << 24) - 8;   // (of a grid of 2^32 threads HIP runs what is left modulo 2^32, without an error)
-constexpr int PACKED_SORTED = 64;            // with more sequences items go by sequence, whole
+// With more sequences items go by sequence, whole: a wave's lanes have a sequence each, once.  64 / 65 sequences, us: one new row of each on 20000 keys, 4 query heads of one KV head 154 / 458, one of 20000
+// among ones of 300, a new row each, 8 KV heads 68 / 332; where the rows fill the chip there is nothing to cut: prompts of 300 and one of 8192 589 / 582.
+constexpr int PACKED_SORTED = 64;
 // How a call cuts its items.  Parts are no more than the workgroups that are resident, so that they run at once (fp32 at d = 128 twice as many: one and two rounds, us, 1024 positions 51.6 / 47.0,
 // 300 and 40 new rows behind 2700 and none 103.5 / 76.6).  Whole / cut, us: follow-ups of 1 to 200 rows on 2900 to 20000 keys 460 / 83, 61 new rows of 12347 216 / 37, fp32 1024 positions of 8 heads of 128 149 / 47.
 struct PackedCut {
