@@ -319,7 +319,8 @@ size_t ls_packed_workspace_bytes(const ls_shape* shape);
  *   pos [B] int32, device memory: the position in the cache at which sequence s's rows begin; NULL: 0.
  * ls_cache_write: bf16 pages hold the rows rounded to nearest even.  E4M3: E is the smallest byte from 10 to 247 with
  *   max |x| <= 448 * 2^(E-127) over the row's finite values, the codes are x * 2^(127-E) rounded to nearest even; infinities and
- *   NaN become NaN.  What else is in the pages stays.  Rows that meet in one place (a page that is twice in the table) leave one of the values of each there.
+ *   NaN become NaN.  What else is in the pages stays.  Of rows that meet in one place (a page that is twice in the table), each value there is one of theirs, and
+ *   the byte E of an e4m3 row may be another row's than its codes.
  * ls_cache_read: rows past count and rows that are nowhere stay as they are.
  * No workspace.
  */

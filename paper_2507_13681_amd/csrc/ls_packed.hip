@@ -288,7 +288,8 @@ __global__ __launch_bounds__(PK_THREADS, (PackCfg<T, D>::RESIDENT)) void packed_
             load_frag_tr(f, at, at + 8 * C::RB);
         }
     };
-    // probabilities on their way to fragments
+    // Weights on their way to fragments: of bf16 inputs they become bf16, half a step of 2^-8 each, as the matrix instruction takes them beside V (fp32 products have a sixteenth of its rate);
+    // the normaliser adds them up as they were.
     struct Probs {
         std::conditional_t<C::F32, float, uint32_t> w[C::F32 ? 16 : 8];
         __device__ void set(int r, float lo, float hi) {   // registers r, r + 1

@@ -298,7 +298,7 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
                 for (int r = 0; r < 8; ++r) x[r] = whole || (16 * (r >> 2) + 4 * q + (r & 3) < left && hf[r >> 2].on) ? x[r] * vp[r] : 0.f;        // (behind the length the bytes may be anything)
             }
             Frag<T> f;
-            pack_frag(f, x);                                           // contraction index 8 q + r <-> key 16 (r / 4) + 4 q + r % 4
+            pack_frag(f, x);                                           // contraction index 8 q + r <-> key 16 (r / 4) + 4 q + r % 4; bf16 as the products with V take it, not in the normaliser
             pf[h] = f.v;
         }
         asm volatile("" : "+v"(vat));
