@@ -253,6 +253,7 @@ size_t ls_decode_workspace_bytes(const ls_shape* shape, int32_t cap, int32_t T);
  * of whole prompts packed one behind the other, rows into and out of the pages, and a token over them.
  * In the attention, logits, softmax references, normalisers and partial results are fp32; of bf16 inputs the softmax weights are rounded to bf16 for their products
  * with V, while the normaliser adds them up unrounded.  Logits may have magnitudes up to 2^30; rows of larger ones may come out as NaN or zeros.
+ * A logit of -inf weighs nothing, and a row that sees no others is as one that sees no key; one of +inf makes its row NaN, as NaN does.
  */
 
 /* Rows of `H` heads of `d` neighbouring values each, as a caller's tensor holds them.  Sequence s's row i of head h begins

@@ -267,3 +267,89 @@ def test_a_row_does_not_depend_on_its_neighbours_logits(Hq, Hkv, d, dtype):
     others = torch.arange(n) != at
     assert torch.equal(got_lse[:, others], lse[:, others]) and torch.equal(got[others], out[others])
     assert not torch.equal(got[at], out[at])
+
+
+N_MOST = 2147483000                                        # the most rows that a call takes
+
+
+def test_the_longest_sequence_of_a_prompt():
+    """A row on as many keys as there can be (all in one place): equal weights, whose number the normaliser counts."""
+    v = torch.exp2(torch.randint(-3, 4, (1, 1, 64)).float()).bfloat16().cuda()
+    q, k = torch.zeros(2, 1, 64, dtype=torch.bfloat16, device="cuda"), torch.ones(1, 1, 64, dtype=torch.bfloat16, device="cuda")
+    shape = binding.make_shape(1, 1, 1, 64, N_MOST, 2, 1, "bf16")
+    out, lse = torch.empty_like(q), torch.empty(1, 2, device="cuda")
+    ctx = binding.Context(workspace=binding.packed_workspace_bytes(shape))
+    print("packed longest", flush=True)
+    ctx.ls_packed_prefill(shape, q, k.expand(N_MOST, 1, 64), v.expand(N_MOST, 1, 64), _i32([0, 2]), _i32([0, N_MOST]), out, lse)
+    torch.cuda.synchronize()
+    assert torch.equal(out, v.expand(2, 1, 64))            # (sums of powers of two: exact)
+    assert (lse.double() - np.log(N_MOST)).abs().max() <= 2.0 ** -20 * np.log(N_MOST)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_the_longest_sequence_of_pages(kind):
+    """A token on as many keys as there can be, all on one page, behind another sequence of 33."""
+    p = pu.pool(np.random.default_rng(48), 1, 1, 256, 64, kind)
+    row = torch.exp2(torch.randint(-3, 4, (64,)).float())
+    if kind == "bf16":
+        p["v"][:] = row.bfloat16()
+    else:
+        p["v"][:], p["v_exp"][:] = row.to(pu.E4M3).view(torch.uint8), 127
+    table = torch.zeros(2, -(-N_MOST // 256), dtype=torch.int32)
+    print("paged longest", kind, flush=True)
+    out, lse, status = _attend(p, torch.zeros(2, 2, 64).bfloat16(), table, [33, N_MOST])
+    assert status == 0 and torch.equal(out, row.bfloat16().expand(2, 2, 64))
+    n = torch.tensor([33.0, N_MOST]).double().log()[:, None]
+    assert ((lse.double() - n).abs() <= 2.0 ** -20 * n).all()
+
+
+def test_as_many_sequences_as_there_can_be():
+    """65535 of them, a row or none each: what a single key gives is its row of V."""
+    B, d = 65535, 64
+    rng = np.random.default_rng(49)
+    lens = [int(x) for x in rng.choice([0, 1], B)]
+    T = sum(lens)
+    q, k, v = (pu.rnd(rng, T, 1, d).cuda() for _ in range(3))
+    starts = _starts(lens).cuda()
+    shape = binding.make_shape(B, 1, 1, d, T, T, 1, "bf16")
+    ctx = binding.Context(workspace=max(binding.packed_workspace_bytes(shape), binding.paged_workspace_bytes(binding.make_shape(B, 1, 1, d, 1, 1, 1, "bf16"))))
+    out = torch.full_like(q, float("nan"))
+    print("many sequences: packed", flush=True)
+    ctx.ls_packed_prefill(shape, q, k, v, starts, starts, out)
+    assert ctx.ls_poll_status() == 0 and torch.equal(out, v)
+    pool = torch.zeros(B, 1, 16, d, dtype=torch.bfloat16, device="cuda")
+    cache = binding.PagedCache(pool, pool.clone())
+    table, pos = torch.from_numpy(rng.permutation(B).astype(np.int32))[:, None].cuda().contiguous(), _i32([0] * B)
+    print("many sequences: pages", flush=True)
+    ctx.ls_cache_write(binding.make_shape(B, 1, 1, d, 1, T, 1, "bf16"), cache, k, v, table, pos, starts)
+    seq = torch.tensor(lens).nonzero()[:, 0].cuda()
+    assert ctx.ls_poll_status() == 0 and torch.equal(cache.v[table[seq, 0].long(), 0, 0], v[:, 0]) and torch.equal(cache.k[table[seq, 0].long(), 0, 0], k[:, 0])
+    token = torch.full((B, 1, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    print("many sequences: tokens", flush=True)
+    ctx.ls_paged_attend(binding.make_shape(B, 1, 1, d, 1, 1, 1, "bf16"), cache, torch.ones_like(token), table, _i32(lens), token)
+    want = torch.zeros_like(token)
+    want[seq] = v
+    assert ctx.ls_poll_status() == 0 and torch.equal(token, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("n,seen", [(70, 50), (70, 69), (70, None), (3000, 5), (3000, None)])
+def test_logits_of_minus_infinity(n, seen, dtype):
+    """They weigh nothing: one finite key gives its row of V, and rows without any are as rows without a key; whole items and parts."""
+    q, k, v = _inputs(50, 4, 1, 64, [n], [3], dtype)
+    q, k[..., 0] = q.abs(), -float("inf")
+    if seen is not None:
+        k[seen, 0, 0] = 1.0
+    print("packed minus infinity", n, seen, dtype, flush=True)
+    out, lse = _run(q, k, v, [n], [3])
+    sees = torch.arange(n - 3, n) >= (n if seen is None else seen)
+    want = torch.where(sees[:, None, None], v[seen or 0], torch.zeros(())).expand(3, 4, 64)
+    assert ((out.double() - want.double()).abs() <= pu.HALF[dtype] * 2.02 * want.double().abs()).all()
+    assert torch.equal(torch.isneginf(lse), ~sees.expand(4, 3)) and not torch.isnan(lse).any()
+    if dtype == torch.bfloat16:
+        pages = -(-n // 16)
+        p = {name: torch.zeros(pages, 1, 16, 64, dtype=dtype) for name in "kv"}
+        p["k"].view(-1, 64)[:n], p["v"].view(-1, 64)[:n] = k[:, 0], v[:, 0]
+        token, tl, status = _attend(p, q[2:], torch.arange(pages, dtype=torch.int32)[None], [n])
+        assert status == 0 and ((token[0].double() - want[2].double()).abs() <= pu.HALF[dtype] * 2.02 * want[2].double().abs()).all()
+        assert torch.isneginf(tl).all() == (seen is None) and not torch.isnan(tl).any()
