@@ -265,7 +265,7 @@ typedef struct {
     int64_t seq, row, head;
 } ls_rows;
 
-typedef enum { LS_CACHE_BF16 = 0, LS_CACHE_E4M3 = 1 } ls_cache_type;
+typedef enum { LS_CACHE_BF16 = 0, LS_CACHE_E4M3 = 1, LS_CACHE_E2M1 = 4 } ls_cache_type;
 
 /* A pool of pages.  Page p holds `page` neighbouring positions of one sequence, of all KV heads: k, v [pages,Hkv,page,d],
  * contiguous, 16-byte aligned.  LS_CACHE_BF16: bf16.  LS_CACHE_E4M3: 8-bit floats (1 sign, 4 exponent, 3 fraction bits, bias 7, no
@@ -273,6 +273,9 @@ typedef enum { LS_CACHE_BF16 = 0, LS_CACHE_E4M3 = 1 } ls_cache_type;
  * for code * 2^(E - 127), and for NaN where E is 255.  ls_cache_write makes E from 10 to 247, of which bf16 and fp32 hold every value exactly (but for
  * 2^128, to which magnitudes from 1.9375 * 2^127 on round: infinity).  Pages that a caller fills may have other bytes: ls_cache_read rounds their values to
  * the rows' type, ls_paged_attend rounds those of K to bf16.  A softmax weight times the power 2^(E - 127) of its row of V is a bf16 there, which has fewer bits below 2^-126.
+ * LS_CACHE_E2M1: 4-bit floats (1 sign, 2 exponent, 1 fraction bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6) in k, v [pages,Hkv,page,d/2], value 2 i of a row in the low half of its byte i, and in
+ * k_exp, v_exp [pages,Hkv,page,d/32] a byte E for each 32 neighbouring values of a row: a stored value stands for code * 2^(E - 127), and for NaN where E is 255.  ls_cache_write makes E
+ * from 2 to 253, of which bf16 and fp32 hold every value exactly (but for 2^128 and 1.5 * 2^128: infinity), and 255.  ls_paged_attend rounds the values of K and of V to bf16.
  * Where a sequence's pages are is a row of `table` [B,max_pages] int32, device memory: positions p * page .. of sequence b lie in
  * page table[b][p].  Several sequences may share pages that are read.  A page number outside [0, pages), and a position beyond max_pages * page, is nowhere:
  * rows of it are neither written nor read, keys of it are not seen, and LS_STAT_PAGE_RANGE is set. */
@@ -282,7 +285,7 @@ typedef struct {
     int32_t type;            /* ls_cache_type */
     int64_t pages;           /* 1 <= pages < 2^31 */
     void *k, *v;
-    uint8_t *k_exp, *v_exp;  /* LS_CACHE_E4M3 only */
+    uint8_t *k_exp, *v_exp;  /* not for LS_CACHE_BF16 */
 } ls_cache;
 
 /*
@@ -320,8 +323,9 @@ size_t ls_packed_workspace_bytes(const ls_shape* shape);
  *   pos [B] int32, device memory: the position in the cache at which sequence s's rows begin; NULL: 0.
  * ls_cache_write: bf16 pages hold the rows rounded to nearest even.  E4M3: E is the smallest byte from 10 to 247 with
  *   max |x| <= 448 * 2^(E-127) over the row's finite values, the codes are x * 2^(127-E) rounded to nearest even; infinities and
- *   NaN become NaN.  What else is in the pages stays.  Of rows that meet in one place (a page that is twice in the table), each value there is one of theirs, and
- *   the byte E of an e4m3 row may be another row's than its codes.
+ *   NaN become NaN.  E2M1: of each 32 values E is the smallest byte from 2 to 253 with max |x| <= 7 * 2^(E-127), the codes are x * 2^(127-E) rounded to the nearest, ties to the one with fraction bit 0, what is
+ *   beyond 6 to 6; 32 values with an infinity or NaN among them become NaN: E is 255 and the codes are 0.  What else is in the pages stays.  Of rows that meet in one place (a page that is twice in the table), each value there is one of theirs, and
+ *   a byte E may be another row's than its codes.
  * ls_cache_read: rows past count and rows that are nowhere stay as they are.
  * No workspace.
  */

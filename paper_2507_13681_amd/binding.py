@@ -26,7 +26,7 @@ ENTRY_POINTS = ("ls_workspace_bytes", "ls_create", "ls_destroy", "ls_last_error"
 # bits of the device status word (ls_poll_status)
 LS_STAT_WALK_TIMEOUT, LS_STAT_S_TRUNCATED, LS_STAT_V_TRUNCATED, LS_STAT_S_RANGE, LS_STAT_V_INVALID = 1, 2, 4, 8, 16
 LS_STAT_MERGE_RANGE, LS_STAT_PAGE_RANGE, LS_STAT_STARTS = 32, 64, 128
-LS_CACHE_BF16, LS_CACHE_E4M3 = 0, 1
+LS_CACHE_BF16, LS_CACHE_E4M3, LS_CACHE_E2M1 = 0, 1, 4
 
 
 class LsShape(C.Structure):
@@ -182,26 +182,31 @@ def paged_workspace_bytes(shape: LsShape) -> int:
 
 
 class PagedCache:
-    """A pool of pages (ls_cache): k, v [pages,Hkv,page,d], bf16, or 8-bit e4m3 codes (torch.uint8 or torch.float8_e4m3fn) with
-    k_exp, v_exp [pages,Hkv,page] uint8.  Holds the tensors, which stay the caller's; stored 8-bit values stand for code * 2^(exp - 127)."""
+    """A pool of pages (ls_cache): k, v [pages,Hkv,page,d], bf16; or 8-bit e4m3 codes (torch.uint8 or torch.float8_e4m3fn) with
+    k_exp, v_exp [pages,Hkv,page] uint8; or 4-bit e2m1 codes, two to a byte, k, v [pages,Hkv,page,d/2] (torch.uint8 or torch.float4_e2m1fn_x2) with k_exp, v_exp [pages,Hkv,page,d/32] uint8.
+    Holds the tensors, which stay the caller's; stored codes stand for code * 2^(exp - 127)."""
 
     def __init__(self, k, v, k_exp=None, v_exp=None):
-        if k.dtype not in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn):
-            raise ValueError("pages are torch.bfloat16, or torch.uint8 or torch.float8_e4m3fn codes")
+        if k.dtype not in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn, torch.float4_e2m1fn_x2):
+            raise ValueError("pages are torch.bfloat16, or torch.uint8, torch.float8_e4m3fn or torch.float4_e2m1fn_x2 codes")
         codes = k.dtype != torch.bfloat16
         if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
             raise ValueError("k and v must be [pages, Hkv, page, d], alike")
         if codes != (k_exp is not None) or codes != (v_exp is not None):
-            raise ValueError("8-bit pages have exponents, and bf16 pages none")
+            raise ValueError("8-bit and 4-bit pages have exponents, and bf16 pages none")
+        four = codes and k_exp.dim() == 4                  # an exponent for each 32 values, and not for a row
+        if codes and four != (k.dtype == torch.float4_e2m1fn_x2) and k.dtype != torch.uint8:
+            raise ValueError("exponents must be [pages, Hkv, page] of 8-bit pages, [pages, Hkv, page, d / 32] of 4-bit ones")
         for e in (k_exp, v_exp) if codes else ():
-            if e.dtype != torch.uint8 or e.shape != k.shape[:3]:
-                raise ValueError("exponents must be [pages, Hkv, page] uint8")
+            if e.dtype != torch.uint8 or e.shape != (k.shape[:3] + (k.shape[3] // 16,) if four else k.shape[:3]):
+                raise ValueError("exponents must be [pages, Hkv, page] uint8, or [pages, Hkv, page, d / 32] of 4-bit pages")
         tensors = [t for t in (k, v, k_exp, v_exp) if t is not None]
         if not all(t.is_cuda and t.is_contiguous() and t.device == k.device for t in tensors):
             raise ValueError("pages must be contiguous tensors of one GPU")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.device = k.device.index
-        self.struct = LsCache(k.shape[1], k.shape[3], k.shape[2], LS_CACHE_E4M3 if codes else LS_CACHE_BF16, k.shape[0], k.data_ptr(), v.data_ptr(),
+        kind = LS_CACHE_E2M1 if four else LS_CACHE_E4M3 if codes else LS_CACHE_BF16
+        self.struct = LsCache(k.shape[1], k.shape[3] * (2 if four else 1), k.shape[2], kind, k.shape[0], k.data_ptr(), v.data_ptr(),
                               k_exp.data_ptr() if codes else None, v_exp.data_ptr() if codes else None)
 
 

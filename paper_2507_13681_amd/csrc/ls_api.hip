@@ -20,6 +20,7 @@ static_assert(ls::STAT_WALK_TIMEOUT == LS_STAT_WALK_TIMEOUT && ls::STAT_S_TRUNCA
               ls::STAT_V_INVALID == LS_STAT_V_INVALID && ls::STAT_MERGE_RANGE == LS_STAT_MERGE_RANGE &&
               ls::STAT_PAGE_RANGE == LS_STAT_PAGE_RANGE && ls::STAT_STARTS == LS_STAT_STARTS,
               "status bits of the kernels and of the header");
+static_assert(ls::CACHE_BF16 == LS_CACHE_BF16 && ls::CACHE_E4M3 == LS_CACHE_E4M3 && ls::CACHE_E2M1 == LS_CACHE_E2M1, "types of pages of the kernels and of the header");
 
 struct ls_ctx {
     int device;
@@ -679,12 +680,12 @@ Wrong check_rows(const ls_rows* r, int dtype, int d, int64_t seqs, int64_t rows,
 }
 Wrong check_cache(const ls_cache* c, const ls_shape* s, const int32_t* table, int32_t max_pages) {
     if (!c) return {LS_EINVAL, "cache is NULL"};
-    if (c->type != LS_CACHE_BF16 && c->type != LS_CACHE_E4M3) return {LS_EINVAL, "cache type must be LS_CACHE_BF16 or LS_CACHE_E4M3"};
+    if (c->type != LS_CACHE_BF16 && c->type != LS_CACHE_E4M3 && c->type != LS_CACHE_E2M1) return {LS_EINVAL, "cache type must be LS_CACHE_BF16, LS_CACHE_E4M3 or LS_CACHE_E2M1"};
     if (c->Hkv != s->Hkv || c->d != s->d) return {LS_ESHAPE, "Hkv and d of the cache and of the shape differ"};
     if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1))) return {LS_ESHAPE, "page must be 16, 32, 64, 128 or 256"};
     if (c->pages < 1 || c->pages > 2147483647LL) return {LS_ESHAPE, "need 1 <= pages < 2^31"};
     if (max_pages < 1) return {LS_ESHAPE, "max_pages must be positive"};
-    const bool e = c->type == LS_CACHE_E4M3;
+    const bool e = c->type != LS_CACHE_BF16;
     if (!c->k || !c->v || !table || (e && (!c->k_exp || !c->v_exp))) return {LS_EINVAL, "NULL tensor"};
     if (!aligned16(c->k) || !aligned16(c->v) || (e && (!aligned16(c->k_exp) || !aligned16(c->v_exp)))) return {LS_EINVAL, "misaligned cache"};
     return FINE;

@@ -1,15 +1,8 @@
 // Rows of K and V into the pages of a cache and back (ls_cache_write, ls_cache_read).
 //
-// A row has d values of one position and KV head.  e4m3 pages hold code = x * 2^(127 - E), rounded to nearest even, with one byte E a row: the least power of
-// two by which the row's largest finite value fits under 448, the largest of e4m3.  A power of two, and not max / 448: the products are exact, so that the
-// only rounding is that of the code, a stored value times its power is a bf16, and the attention over it needs no scaled products; what it costs is at most one of the
-// fifteen binades of e4m3 below a row's largest value.
-//
 // Bound by memory: each row is read and written once, and of each position the table's entry.  8 KV heads of 128, e4m3, us: 32768 bf16 rows written 43 (4.7 TB/s, read and written), four caches of
 // 16384 read back 79 (5.1 TB/s; a copy of 1 GiB reaches 5.15); one row of each of four sequences written 4.6, where an empty launch is 2.6.
-#include <type_traits>
-#include "ls_device.h"
-#include "ls_internal.h"
+#include "ls_rows.h"
 
 namespace ls {
 
@@ -21,43 +14,6 @@ constexpr int64_t ON_CHIP = 256 << 20;
 // Workgroups of a launch.  A dimension of a grid has less than 2^32 threads: of one that has more, HIP runs what is left of the number modulo 2^32, and says nothing.
 constexpr int64_t MOVE_GROUPS = 1 << 23;
 
-// Largest over the LPR (8 or 16) neighbouring lanes of a row
-template <int LPR>
-__device__ __forceinline__ float row_largest(float x) {
-    auto with = [](float v, auto ctrl) {
-        return fmaxf(v, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, false)));
-    };
-    x = with(x, std::integral_constant<int, 0xB1>{});      // quad_perm 1,0,3,2
-    x = with(x, std::integral_constant<int, 0x4E>{});      // quad_perm 2,3,0,1
-    x = with(x, std::integral_constant<int, 0x141>{});     // row_half_mirror
-    if (LPR == 16) x = with(x, std::integral_constant<int, 0x140>{});                        // row_mirror
-    return x;
-}
-// The exponent byte of a row whose largest finite value is x >= 0: 448 is 1.75 * 2^8
-__device__ __forceinline__ uint32_t row_exponent(float x) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, x);
-    const int e = (int)(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return e > 10 ? (uint32_t)e : 10u;                     // (below, the smallest code would be no normal bf16)
-}
-__device__ __forceinline__ float power_of(uint32_t E) { return __builtin_bit_cast(float, E << 23); }        // 2^(E - 127)
-
-// Eight neighbouring values of a row, as they come and as floats
-template <typename T> struct Eight;
-template <> struct Eight<bf16_t> {
-    bf16x8 v;
-    __device__ void load(const unsigned char* p) { v = *reinterpret_cast<const bf16x8*>(p); }
-    __device__ void store(unsigned char* p) const { *reinterpret_cast<bf16x8*>(p) = v; }
-    __device__ float at(int i) const { return (float)v[i]; }
-    __device__ void set(int i, float x) { v[i] = (__bf16)x; }
-};
-template <> struct Eight<float> {
-    f32x4 v[2];
-    __device__ void load(const unsigned char* p) { v[0] = reinterpret_cast<const f32x4*>(p)[0]; v[1] = reinterpret_cast<const f32x4*>(p)[1]; }
-    __device__ void store(unsigned char* p) const { reinterpret_cast<f32x4*>(p)[0] = v[0]; reinterpret_cast<f32x4*>(p)[1] = v[1]; }
-    __device__ float at(int i) const { return v[i / 4][i % 4]; }
-    __device__ void set(int i, float x) { v[i / 4][i % 4] = x; }
-};
-
 // Loads by f(load) of what is wanted once (`once`, wave-uniform) or again.  The empty statements keep the two sides apart: joined, all would be ordinary loads.
 template <typename F>
 __device__ __forceinline__ void load_by(bool once, F f) {
@@ -67,9 +23,9 @@ __device__ __forceinline__ void load_by(bool once, F f) {
 
 // grid (blocks of rows, groups of KV heads).  A workgroup has 256 / (d / 8) neighbouring rows, and of a row d / 8 lanes eight values each: whose sequence each
 // row is of, and the place that the table gives it, are found once for all its heads and for K and V.
-template <bool WRITE, typename T, bool E4M3, int D>
+template <bool WRITE, typename T, int TYPE, int D>
 __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
-    constexpr int LPR = D / 8, ROWS = MOVE_THREADS / LPR, SRC = Elem<T>::bytes, DST = E4M3 ? 1 : 2;
+    constexpr int LPR = D / 8, ROWS = MOVE_THREADS / LPR, SRC = Elem<T>::bytes;
     __shared__ int seq_s[ROWS], stop_s;
     const int tid = threadIdx.x, slot = tid / LPR, part = tid % LPR;
     const int64_t row0 = (a.group0 + blockIdx.x) * ROWS;
@@ -116,28 +72,8 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
     unsigned char* const pool[2] = {a.cache.k, a.cache.v};
     uint8_t* const exps[2] = {a.cache.kx, a.cache.vx};
     auto put = [&](const Eight<T>& x, int h, int t) {      // into the cache
-        const int64_t r = place + ((int64_t)h << a.cache.page_log);
-        unsigned char* dst = pool[t] + r * (D * DST) + 8 * part * DST;
-        if constexpr (E4M3) {
-            float m = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { const float y = fabsf(x.at(e)); m = fmaxf(m, y < INFINITY ? y : 0.f); }
-            const uint32_t E = row_exponent(row_largest<LPR>(m));
-            const float f = power_of(254u - E);
-            uint32_t w[2] = {0u, 0u};
-#pragma unroll
-            for (int e = 0; e < 8; e += 4) {
-                int u = __builtin_amdgcn_cvt_pk_fp8_f32(x.at(e) * f, x.at(e + 1) * f, 0, false);
-                w[e / 4] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x.at(e + 2) * f, x.at(e + 3) * f, u, true);
-            }
-            *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-            if (part == 0) exps[t][r] = (uint8_t)E;
-        } else {
-            Eight<bf16_t> y;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y.set(e, x.at(e));
-            y.store(dst);
-        }
+        const Eight<T> one[1] = {x};
+        store_part<TYPE, D, 8>(one, pool[t], exps[t], place + ((int64_t)h << a.cache.page_log), part);
     };
     if constexpr (WRITE) {
         int h = h0;
@@ -154,8 +90,11 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
     } else {
         auto get = [&](auto load, int h, int t, uint2& w, Eight<bf16_t>& x, uint32_t& E) {
             const int64_t r = place + ((int64_t)h << a.cache.page_log);
-            const unsigned char* src = pool[t] + r * (D * DST) + 8 * part * DST;
-            if constexpr (E4M3) {
+            const unsigned char* src = pool[t] + r * stored_bytes(TYPE, D) + part * stored_bytes(TYPE, 8);
+            if constexpr (TYPE == CACHE_E2M1) {
+                w.x = load(reinterpret_cast<const uint32_t*>(src));
+                E = exps[t][r * (D / 32) + part / 4];
+            } else if constexpr (TYPE == CACHE_E4M3) {
                 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
                 const u32x2 y = load(reinterpret_cast<const u32x2*>(src));
                 w = make_uint2(y.x, y.y);
@@ -166,7 +105,20 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
         };
         auto give = [&](int h, int t, const uint2& w, const Eight<bf16_t>& x, uint32_t E) {
             Eight<T> y;
-            if constexpr (E4M3) {
+            if constexpr (TYPE == CACHE_E2M1) {
+                const float f = power_of(E);
+                auto two = [&](auto i) {                   // byte i's
+                    constexpr int I = decltype(i)::value;
+                    if constexpr (std::is_same<T, float>::value) {
+                        const auto z = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.x, f, I);
+                        y.set(2 * I, z[0]); y.set(2 * I + 1, z[1]);
+                    } else {
+                        const auto z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w.x, f, I);
+                        y.set(2 * I, (float)z[0]); y.set(2 * I + 1, (float)z[1]);
+                    }
+                };
+                two(std::integral_constant<int, 0>{}); two(std::integral_constant<int, 1>{}); two(std::integral_constant<int, 2>{}); two(std::integral_constant<int, 3>{});
+            } else if constexpr (TYPE == CACHE_E4M3) {
                 const float f = power_of(E);               // (of which a conversion looks at the exponent alone: 2^-127 for 0, and NaN comes of 255)
                 const uint32_t u[2] = {w.x, w.y};
 #pragma unroll
@@ -203,19 +155,19 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
     }
 }
 
-template <bool WRITE, typename T, bool E4M3, int D>
+template <bool WRITE, typename T, int TYPE, int D>
 static hipError_t run_move_t(MoveArgs a, hipStream_t st) {
-    constexpr int ROWS = MOVE_THREADS / (D / 8), BYTES = Elem<T>::bytes + (E4M3 ? 1 : 2);
+    constexpr int ROWS = MOVE_THREADS / (D / 8), BYTES = D * Elem<T>::bytes + stored_bytes(TYPE, D);
     const int64_t rows = (a.starts ? 1 : (int64_t)a.B) * a.n_hat;
     const int64_t blocks = (rows + ROWS - 1) / ROWS;
     // All heads of a row in one workgroup where there are rows enough: what a row is and where it goes is found once for them.  Two heads of them otherwise, for more workgroups.  All heads / two, us:
     // four caches of 16384 (their pages through the caches), packed 81 / 86, padded 81 / 79, 16384 rows of 32 heads of 64 49 / 51, four single rows 5.5 / 4.7, 3400 rows of fp32 5.8 / 5.4.
     a.heads = a.cache.Hkv;
     while (a.heads > 2 && blocks * ((a.cache.Hkv + a.heads - 1) / a.heads) < 2048) a.heads = (a.heads + 1) / 2;
-    a.once = rows * a.cache.Hkv * (2 * D * BYTES) > ON_CHIP;
+    a.once = rows * a.cache.Hkv * (2 * BYTES) > ON_CHIP;
     for (a.group0 = 0; a.group0 < blocks; a.group0 += MOVE_GROUPS) {
         const int64_t here = blocks - a.group0 < MOVE_GROUPS ? blocks - a.group0 : MOVE_GROUPS;
-        hipLaunchKernelGGL((move_kernel<WRITE, T, E4M3, D>), dim3((uint32_t)here, (a.cache.Hkv + a.heads - 1) / a.heads), dim3(MOVE_THREADS), 0, st, a);
+        hipLaunchKernelGGL((move_kernel<WRITE, T, TYPE, D>), dim3((uint32_t)here, (a.cache.Hkv + a.heads - 1) / a.heads), dim3(MOVE_THREADS), 0, st, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -223,8 +175,9 @@ static hipError_t run_move_t(MoveArgs a, hipStream_t st) {
 }
 template <bool WRITE, typename T>
 static hipError_t run_move_d(const MoveArgs& a, int type, int d, hipStream_t st) {
-    if (type) return d == 128 ? run_move_t<WRITE, T, true, 128>(a, st) : run_move_t<WRITE, T, true, 64>(a, st);
-    return d == 128 ? run_move_t<WRITE, T, false, 128>(a, st) : run_move_t<WRITE, T, false, 64>(a, st);
+    if (type == CACHE_E2M1) return d == 128 ? run_move_t<WRITE, T, CACHE_E2M1, 128>(a, st) : run_move_t<WRITE, T, CACHE_E2M1, 64>(a, st);
+    if (type == CACHE_E4M3) return d == 128 ? run_move_t<WRITE, T, CACHE_E4M3, 128>(a, st) : run_move_t<WRITE, T, CACHE_E4M3, 64>(a, st);
+    return d == 128 ? run_move_t<WRITE, T, CACHE_BF16, 128>(a, st) : run_move_t<WRITE, T, CACHE_BF16, 64>(a, st);
 }
 hipError_t run_move(const MoveArgs& a, bool write, int dtype, int type, int d, hipStream_t st) {
     if (write) return dtype == 0 ? run_move_d<true, bf16_t>(a, type, d, st) : run_move_d<true, float>(a, type, d, st);

@@ -169,10 +169,11 @@ struct DecodeArgs {
     float scale_log2e;
 };
 
-// A paged cache (ls_cache)
+// A paged cache (ls_cache); types are mirrors of ls_cache_type
+constexpr int CACHE_BF16 = 0, CACHE_E4M3 = 1, CACHE_E2M1 = 4;
 struct CacheArgs {
-    unsigned char *k, *v;     // [pages][Hkv][page][d] bf16 or e4m3
-    uint8_t *kx, *vx;         // [pages][Hkv][page] e4m3: exponents
+    unsigned char *k, *v;     // [pages][Hkv][page][d] bf16 or e4m3, or [..][d / 2] bytes of two e2m1 codes
+    uint8_t *kx, *vx;         // exponents: e4m3 [pages][Hkv][page], e2m1 [..][d / 32]
     const int32_t* table;     // [B][max_pages]
     int max_pages;
     uint32_t pages;
@@ -352,6 +353,9 @@ PackedCut packed_cut(int B, bool packed, int64_t keys, int64_t queries, int Hkv,
 int64_t packed_items(int B, int64_t n_hat, int Hkv, int G, bool packed);       // no fewer than there are
 hipError_t run_move(const MoveArgs& a, bool write, int dtype, int type, int d, hipStream_t st);
 hipError_t run_paged(const PagedArgs& a, int type, int d, int units, hipStream_t st);
+hipError_t init_paged4_kernels();
+hipError_t run_paged4(const PagedArgs& a, int d, int units, hipStream_t st);                 // run_paged of e2m1 pages
+void launch_paged_join(const PagedArgs& a, int d, hipStream_t st);
 int paged_units(int B, int Hkv, int64_t most);                       // workgroups that sequences of up to so many keys take
 bool paged_joins(int B, int Hkv, int G, int64_t most);                      // the kernel puts parts together itself
 int paged_most_cuts(int B, int Hkv, int64_t most);                   // ... and parts of a head
