@@ -336,6 +336,35 @@ int ls_cache_read(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, con
                   const int32_t* starts, const int32_t* count, const int32_t* table, int32_t max_pages,
                   const int32_t* pos, void* hip_stream);
 
+/* The norms and the rotation that ls_norm_rotate gives queries and keys.  Device memory, fp32, 16-byte aligned. */
+typedef enum { LS_PAIRS_HALVES = 0, LS_PAIRS_NEIGHBOURS = 1 } ls_pairs;
+typedef struct {
+    const float* freq;                   /* [dims/2] radians a position; NULL allowed when dims == 0 */
+    const float *q_weight, *k_weight;    /* [d], or NULL: that tensor's rows are not normed */
+    int32_t dims;                        /* the first `dims` values of a row are rotated: a multiple of 16, at most d */
+    int32_t pairs;                       /* ls_pairs: value i with value i + dims/2, or values 2 i and 2 i + 1 */
+    float eps;                           /* >= 0 */
+} ls_rotation;
+
+/*
+ * ls_norm_rotate -- what q and k are given between their projection and the attention, in one pass: each head's row becomes
+ *     y = x / sqrt(mean(x^2) + eps) * weight,
+ * and of its first `dims` values each pair (a, b) number i is turned by t = position * freq[i]: (a cos t - b sin t, b cos t + a sin t).
+ *
+ *   shape: Hq, Hkv, d, dtype, n_hat; B sequences of n_hat rows each (packed sequences, however many, are one: B = 1).  n, w, scale are ignored.
+ *   q [Hq], k [Hkv heads] as ls_rows;  positions [B,n_hat] int32, device memory, or NULL: row i of a sequence is at position i
+ * Outputs:
+ *   q_out as ls_rows; k_out as ls_rows, or NULL where keys go into a cache only.  They may be q and k themselves (the same strides), and overlap nothing else that is read.
+ *   cache, v, slots (together, or all NULL): the keys, rounded to dtype, and the rows of v as they are go into the cache's pages as ls_cache_write has it: row i to slot
+ *        slots[i] = page * (positions of a page) + place in it ([B,n_hat] int64, device memory, e.g. of ls_cache_resize).  A negative slot is nowhere; one beyond the pool
+ *        too, with LS_STAT_PAGE_RANGE.  Of rows with one slot, each value there is one of theirs.
+ * Sums are fp32, or 64 bits where squares leave its range; the angle is formed in 64 bits (up to |t| = 2^31 its sine and cosine are off by no more than 2^-21), and results are rounded once.
+ * No workspace.
+ */
+int ls_norm_rotate(ls_ctx* ctx, const ls_shape* shape, const ls_rotation* rotation, const ls_rows* q, const ls_rows* k,
+                   const int32_t* positions, const ls_rows* q_out, const ls_rows* k_out,
+                   const ls_cache* cache, const ls_rows* v, const int64_t* slots, void* hip_stream);
+
 /*
  * ls_paged_attend -- ls_decode_attend over pages: the newest token's query of each sequence attends over the first len[b]
  * positions of its cache.
@@ -382,7 +411,7 @@ int ls_profile_prefill_kernel_ms(ls_ctx* ctx, double* mean_ms, int32_t* launches
 #define LS_STAT_V_INVALID   16  /* ls_sparse_prefill: a head's v_idx was not strictly ascending inside [0, n); that
                                    head's columns were ignored (its diagonals still apply) */
 #define LS_STAT_MERGE_RANGE 32  /* ls_merge_lines: input entries outside [0, n) were dropped */
-#define LS_STAT_PAGE_RANGE  64  /* ls_cache_write, ls_cache_read, ls_paged_attend: a position lies in no page of the pool or beyond
+#define LS_STAT_PAGE_RANGE  64  /* ls_cache_write, ls_cache_read, ls_norm_rotate, ls_paged_attend: a position lies in no page of the pool or beyond
                                    the table; it was left out */
 #define LS_STAT_STARTS     128  /* ls_packed_prefill, ls_cache_write, ls_cache_read: a sequence's starts descend or leave the rows;
                                    it was passed by, with all behind it */

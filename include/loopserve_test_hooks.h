@@ -80,6 +80,9 @@ int ls_debug_check_move(const ls_shape* shape, const ls_cache* cache, const ls_r
 int ls_debug_check_paged(const ls_shape* shape, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages, const int32_t* len,
                          const void* out, const float* lse);
 
+int ls_debug_check_rotate(const ls_shape* shape, const ls_rotation* rotation, const ls_rows* q, const ls_rows* k, const int32_t* positions, const ls_rows* q_out,
+                          const ls_rows* k_out, const ls_cache* cache, const ls_rows* v, const int64_t* slots);
+
 /* The page (of `pages` of `page` positions) that the kernels take position `pos` of sequence b to lie in, -1 for none; `table` is host memory here. */
 int ls_debug_page_of(const int32_t* table, int32_t max_pages, int64_t pages, int32_t page, int32_t b, int64_t pos);
 

@@ -27,6 +27,7 @@ ENTRY_POINTS = ("ls_workspace_bytes", "ls_create", "ls_destroy", "ls_last_error"
 LS_STAT_WALK_TIMEOUT, LS_STAT_S_TRUNCATED, LS_STAT_V_TRUNCATED, LS_STAT_S_RANGE, LS_STAT_V_INVALID = 1, 2, 4, 8, 16
 LS_STAT_MERGE_RANGE, LS_STAT_PAGE_RANGE, LS_STAT_STARTS = 32, 64, 128
 LS_CACHE_BF16, LS_CACHE_E4M3, LS_CACHE_E2M1 = 0, 1, 4
+LS_PAIRS_HALVES, LS_PAIRS_NEIGHBOURS = 0, 1
 
 
 class LsShape(C.Structure):
@@ -42,6 +43,10 @@ class LsCache(C.Structure):
 
 class LsRows(C.Structure):
     _fields_ = [("data", C.c_void_p), ("seq", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class LsRotation(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("dims", C.c_int32), ("pairs", C.c_int32), ("eps", C.c_float)]
 
 
 class LoopServeError(RuntimeError):
@@ -106,6 +111,11 @@ def load_library():
     lib.ls_debug_check_move.argtypes = [sp, cp, rp, rp, vp, vp, vp, i32, vp, i32]
     lib.ls_debug_check_paged.restype = C.c_int
     lib.ls_debug_check_paged.argtypes = [sp, cp, vp, vp, i32, vp, vp, vp]
+    tp = C.POINTER(LsRotation)
+    lib.ls_norm_rotate.restype = C.c_int
+    lib.ls_norm_rotate.argtypes = [vp, sp, tp, rp, rp, vp, rp, rp, cp, rp, vp, vp]
+    lib.ls_debug_check_rotate.restype = C.c_int
+    lib.ls_debug_check_rotate.argtypes = [sp, tp, rp, rp, vp, rp, rp, cp, rp, vp]
     lib.ls_debug_page_of.restype = C.c_int
     lib.ls_debug_page_of.argtypes = [C.POINTER(i32), i32, i64, i32, i32, i64]
     lib.ls_debug_packed_counts.restype = C.c_int
@@ -208,6 +218,23 @@ class PagedCache:
         kind = LS_CACHE_E2M1 if four else LS_CACHE_E4M3 if codes else LS_CACHE_BF16
         self.struct = LsCache(k.shape[1], k.shape[3] * (2 if four else 1), k.shape[2], kind, k.shape[0], k.data_ptr(), v.data_ptr(),
                               k_exp.data_ptr() if codes else None, v_exp.data_ptr() if codes else None)
+
+
+class Rotation:
+    """The norms and the rotation of a model's queries and keys (ls_rotation): freq [dims/2] fp32, radians a position (None: no rotation); q_weight, k_weight [d] fp32
+    or None: not normed; neighbours: values 2 i and 2 i + 1 are a pair, and not i and i + dims/2.  Holds the tensors, which stay the caller's."""
+
+    def __init__(self, freq=None, neighbours=False, q_weight=None, k_weight=None, eps=1e-6):
+        tensors = [t for t in (freq, q_weight, k_weight) if t is not None]
+        for t in tensors:
+            if t.dtype != torch.float32 or t.dim() != 1 or not t.is_cuda or not t.is_contiguous() or t.device != tensors[0].device:
+                raise ValueError("freq and weights must be contiguous fp32 vectors of one GPU")
+        self.freq, self.q_weight, self.k_weight = freq, q_weight, k_weight
+        self.device = tensors[0].device.index if tensors else None
+        self.d = {t.shape[0] for t in (q_weight, k_weight) if t is not None}
+        at = lambda t: None if t is None else t.data_ptr()
+        self.struct = LsRotation(at(freq), at(q_weight), at(k_weight), 0 if freq is None else 2 * freq.shape[0],
+                                 LS_PAIRS_NEIGHBOURS if neighbours else LS_PAIRS_HALVES, float(eps))
 
 
 def _ptr(t):
@@ -325,6 +352,17 @@ class Context:
     def ls_cache_read(self, shape, cache, table, k, v, pos=None, starts=None, count=None):
         """k, v: where the rows go."""
         rc = self.pages.cache_read(self.hv, self.device, shape, self._pages(cache), k, v, table, pos, starts, count)
+        if rc:
+            self._check(rc)
+
+    def ls_norm_rotate(self, shape, rotation, q, k, q_out, k_out=None, positions=None, cache=None, v=None, slots=None):
+        """k_out None: keys go into the cache only.  cache, v, slots together, or none of them."""
+        if rotation.device not in (None, self.device):
+            raise ValueError("the rotation is not on the context's GPU")
+        if rotation.d and rotation.d != {shape.d}:
+            raise ValueError("weights must have d values")
+        rc = self.pages.norm_rotate(self.hv, self.device, shape, rotation.struct, q, k, q_out, k_out, positions,
+                                    None if cache is None else self._pages(cache), v, slots)
         if rc:
             self._check(rc)
 

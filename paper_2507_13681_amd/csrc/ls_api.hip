@@ -678,16 +678,22 @@ Wrong check_rows(const ls_rows* r, int dtype, int d, int64_t seqs, int64_t rows,
     }
     return FINE;
 }
-Wrong check_cache(const ls_cache* c, const ls_shape* s, const int32_t* table, int32_t max_pages) {
+Wrong check_pool(const ls_cache* c, const ls_shape* s) {
     if (!c) return {LS_EINVAL, "cache is NULL"};
     if (c->type != LS_CACHE_BF16 && c->type != LS_CACHE_E4M3 && c->type != LS_CACHE_E2M1) return {LS_EINVAL, "cache type must be LS_CACHE_BF16, LS_CACHE_E4M3 or LS_CACHE_E2M1"};
     if (c->Hkv != s->Hkv || c->d != s->d) return {LS_ESHAPE, "Hkv and d of the cache and of the shape differ"};
     if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1))) return {LS_ESHAPE, "page must be 16, 32, 64, 128 or 256"};
     if (c->pages < 1 || c->pages > 2147483647LL) return {LS_ESHAPE, "need 1 <= pages < 2^31"};
-    if (max_pages < 1) return {LS_ESHAPE, "max_pages must be positive"};
     const bool e = c->type != LS_CACHE_BF16;
-    if (!c->k || !c->v || !table || (e && (!c->k_exp || !c->v_exp))) return {LS_EINVAL, "NULL tensor"};
+    if (!c->k || !c->v || (e && (!c->k_exp || !c->v_exp))) return {LS_EINVAL, "NULL tensor"};
     if (!aligned16(c->k) || !aligned16(c->v) || (e && (!aligned16(c->k_exp) || !aligned16(c->v_exp)))) return {LS_EINVAL, "misaligned cache"};
+    return FINE;
+}
+Wrong check_cache(const ls_cache* c, const ls_shape* s, const int32_t* table, int32_t max_pages) {
+    const Wrong w = check_pool(c, s);
+    if (w.code) return w;
+    if (max_pages < 1) return {LS_ESHAPE, "max_pages must be positive"};
+    if (!table) return {LS_EINVAL, "NULL tensor"};
     return FINE;
 }
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -723,6 +729,27 @@ int cache_move(ls_ctx* c, const char* who, bool write, const ls_shape* s, const 
     const hipError_t e = ls::run_move(a, write, s->dtype, cache->type, s->d, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail(c, LS_EHIP, "%s: %s", who, hipGetErrorString(e));
     return LS_OK;
+}
+
+Wrong check_rotate(const ls_shape* s, const ls_rotation* r, const ls_rows* q, const ls_rows* k, const int32_t* positions, const ls_rows* q_out, const ls_rows* k_out,
+                   const ls_cache* cache, const ls_rows* v, const int64_t* slots) {
+    Wrong w = check_heads(s, true);
+    if (w.code) return w;
+    if (s->n_hat < 1 || s->n_hat > MOST_ROWS || s->B * s->n_hat > MOST_ROWS) return {LS_ESHAPE, "rows out of range"};
+    if (!r) return {LS_EINVAL, "rotation is NULL"};
+    if (r->pairs != LS_PAIRS_HALVES && r->pairs != LS_PAIRS_NEIGHBOURS) return {LS_EINVAL, "pairs must be LS_PAIRS_HALVES or LS_PAIRS_NEIGHBOURS"};
+    if (r->dims < 0 || r->dims > s->d || r->dims % 16) return {LS_ESHAPE, "dims must be a multiple of 16 up to d"};
+    if (r->dims && !r->freq) return {LS_EINVAL, "NULL tensor"};
+    if (!aligned16(r->freq) || !aligned16(r->q_weight) || !aligned16(r->k_weight)) return {LS_EINVAL, "misaligned rotation"};
+    if (!(r->eps >= 0.f && r->eps <= 3.402823466e38f)) return {LS_EINVAL, "eps must be a number, not negative"};
+    if (!k_out && !cache) return {LS_EINVAL, "keys go to rows or into a cache"};
+    if (!v != !cache || !slots != !cache) return {LS_EINVAL, "v and slots go with a cache"};
+    if ((reinterpret_cast<uintptr_t>(positions) & 3u) || (reinterpret_cast<uintptr_t>(slots) & 7u)) return {LS_EINVAL, "misaligned index tensor"};
+    if (cache && (w = check_pool(cache, s)).code) return w;
+    if ((w = check_rows(q, s->dtype, s->d, s->B, s->n_hat, s->Hq, false)).code || (w = check_rows(k, s->dtype, s->d, s->B, s->n_hat, s->Hkv, false)).code ||
+        (w = check_rows(q_out, s->dtype, s->d, s->B, s->n_hat, s->Hq, true)).code) return w;
+    if (k_out && (w = check_rows(k_out, s->dtype, s->d, s->B, s->n_hat, s->Hkv, true)).code) return w;
+    return v ? check_rows(v, s->dtype, s->d, s->B, s->n_hat, s->Hkv, false) : FINE;
 }
 
 Wrong check_paged_shape(const ls_shape* s) {
@@ -779,6 +806,24 @@ int ls_cache_write(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const ls
 int ls_cache_read(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const ls_rows* k, const ls_rows* v, const int32_t* starts,
                   const int32_t* count, const int32_t* table, int32_t max_pages, const int32_t* pos, void* stream) {
     return cache_move(c, "ls_cache_read", false, s, cache, k, v, starts, count, table, max_pages, pos, stream);
+}
+
+int ls_norm_rotate(ls_ctx* c, const ls_shape* s, const ls_rotation* r, const ls_rows* q, const ls_rows* k, const int32_t* positions,
+                   const ls_rows* q_out, const ls_rows* k_out, const ls_cache* cache, const ls_rows* v, const int64_t* slots, void* stream) {
+    if (!c) return LS_EINVAL;
+    if (const Wrong w = check_rotate(s, r, q, k, positions, q_out, k_out, cache, v, slots); w.code) return fail(c, w.code, "ls_norm_rotate: %s", w.what);
+    ls::RotateArgs a{};
+    a.q = row_args(q); a.k = row_args(k); a.q_out = row_args(q_out);
+    if (k_out) a.k_out = row_args(k_out);
+    if (cache) { a.cache = cache_args(cache, nullptr, 0); a.v = row_args(v); }
+    a.positions = positions; a.slots = slots;
+    a.freq = r->freq; a.q_weight = r->q_weight; a.k_weight = r->k_weight; a.dims = r->dims; a.neighbours = r->pairs == LS_PAIRS_NEIGHBOURS; a.eps = r->eps;
+    a.B = s->B; a.n_hat = (int)s->n_hat; a.Hq = s->Hq; a.Hkv = s->Hkv; a.status = c->status;
+    const OnDevice on(c->device);
+    if (!on.ok) return fail(c, LS_EHIP, "ls_norm_rotate: hipSetDevice failed");
+    const hipError_t e = ls::run_rotate(a, s->dtype, cache ? cache->type : -1, s->d, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(c, LS_EHIP, "ls_norm_rotate: %s", hipGetErrorString(e));
+    return LS_OK;
 }
 
 size_t ls_packed_workspace_bytes(const ls_shape* s) {
@@ -1001,6 +1046,10 @@ int ls_debug_check_move(const ls_shape* s, const ls_cache* cache, const ls_rows*
 int ls_debug_check_paged(const ls_shape* s, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages, const int32_t* len,
                          const void* out, const float* lse) {
     return check_paged(s, cache, q, table, max_pages, len, out, lse).code;
+}
+int ls_debug_check_rotate(const ls_shape* s, const ls_rotation* r, const ls_rows* q, const ls_rows* k, const int32_t* positions, const ls_rows* q_out,
+                          const ls_rows* k_out, const ls_cache* cache, const ls_rows* v, const int64_t* slots) {
+    return check_rotate(s, r, q, k, positions, q_out, k_out, cache, v, slots).code;
 }
 int ls_debug_page_of(const int32_t* table, int32_t max_pages, int64_t pages, int32_t page, int32_t b, int64_t pos) {
     ls::CacheArgs a{};

@@ -11,8 +11,6 @@ constexpr int MOVE_THREADS = 256;
 // us: four caches of 16384 e4m3 246 -> 233, bf16 268 -> 249; of less data, which the next call may still find there, 16384 rows to fp32 94 for 87 where the same pages are read again.
 // Rows that a call writes, or reads from the caller's tensor, never pass it by: 32768 rows read back would take 32 instead of 42 us, and with a call that reads them 131 instead of 123.
 constexpr int64_t ON_CHIP = 256 << 20;
-// Workgroups of a launch.  A dimension of a grid has less than 2^32 threads: of one that has more, HIP runs what is left of the number modulo 2^32, and says nothing.
-constexpr int64_t MOVE_GROUPS = 1 << 23;
 
 // Loads by f(load) of what is wanted once (`once`, wave-uniform) or again.  The empty statements keep the two sides apart: joined, all would be ordinary loads.
 template <typename F>

@@ -205,6 +205,20 @@ struct MoveArgs {
     int32_t* status;
 };
 
+struct RotateArgs {
+    RowArgs q, k, v, q_out, k_out;             // k_out.data null: keys go into pages only
+    CacheArgs cache;
+    const int32_t* positions;                  // [B][n_hat], null: a row's number
+    const int64_t* slots;                      // [B][n_hat]
+    const float *freq, *q_weight, *k_weight;   // [dims / 2], [d] or null
+    int dims, neighbours;
+    float eps;
+    int B, n_hat, Hq, Hkv;
+    int heads, splits;        // of a row in all, V's among them; groups of lanes that a row's heads are shared out among
+    int64_t group0;           // first workgroup of this launch
+    int32_t* status;
+};
+
 // ls_paged_attend.  A unit of work is a part of the 32-key tiles of one KV head of one sequence, and a workgroup has one.  Which one follows from the lengths, which only the device
 // knows.
 constexpr int PAGED_TILE = 32;               // keys
@@ -352,6 +366,7 @@ hipError_t run_packed(const PackedArgs& a, int dtype, int d, hipStream_t st);
 PackedCut packed_cut(int B, bool packed, int64_t keys, int64_t queries, int Hkv, int G, int dtype, int d, int64_t room);           // with room for so many parts' results
 int64_t packed_items(int B, int64_t n_hat, int Hkv, int G, bool packed);       // no fewer than there are
 hipError_t run_move(const MoveArgs& a, bool write, int dtype, int type, int d, hipStream_t st);
+hipError_t run_rotate(const RotateArgs& a, int dtype, int type, int d, hipStream_t st);         // type -1: no pages
 hipError_t run_paged(const PagedArgs& a, int type, int d, int units, hipStream_t st);
 hipError_t init_paged4_kernels();
 hipError_t run_paged4(const PagedArgs& a, int d, int units, hipStream_t st);                 // run_paged of e2m1 pages

@@ -136,6 +136,27 @@ PyObject* move(PyObject* const* a, Py_ssize_t nargs, F call) {                  
 }
 PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t nargs) { return move(a, nargs, ls_cache_write); }
 PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t nargs) { return move(a, nargs, ls_cache_read); }
+PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t nargs) {           // ctx, device, shape, rotation, q, k, q_out, k_out, positions, cache, v, slots
+    return guarded([&] {
+        Call c(a, nargs, 12);
+        ls_shape& s = c.sh;
+        const ls_rotation r = struct_of<ls_rotation>(a[3], "LsRotation");
+        const bool packed = THPVariable_Check(a[4]) && THPVariable_Unpack(a[4]).dim() == 3;
+        if (packed) s.B = 1;
+        auto rows = [&](int i, const char* name, int64_t H) { return rows_of(a[i], name, s, c.device, packed, s.n_hat, H); };
+        const bool keeps = a[7] != Py_None, pages = a[9] != Py_None;
+        if (pages != (a[10] != Py_None) || pages != (a[11] != Py_None)) wrong("cache", "goes with v and slots");
+        const ls_rows q = rows(4, "q", s.Hq), k = rows(5, "k", s.Hkv), q_out = rows(6, "q_out", s.Hq), k_out = keeps ? rows(7, "k_out", s.Hkv) : ls_rows{};
+        const ls_rows v = pages ? rows(10, "v", s.Hkv) : ls_rows{};
+        const ls_cache cache = pages ? struct_of<ls_cache>(a[9], "LsCache") : ls_cache{};
+        auto index = [&](int i, const char* name, at::ScalarType type) { return packed ? plain(a[i], name, type, c.device, {s.n_hat}) : plain(a[i], name, type, c.device, {s.B, s.n_hat}); };
+        const int32_t* positions = static_cast<int32_t*>(index(8, "positions", I32));
+        const int64_t* slots = static_cast<int64_t*>(index(11, "slots", at::kLong));
+        return released([&] {
+            return ls_norm_rotate(c.ctx, &s, &r, &q, &k, positions, &q_out, keeps ? &k_out : nullptr, pages ? &cache : nullptr, pages ? &v : nullptr, slots, c.stream);
+        });
+    });
+}
 PyObject* paged_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {          // ctx, device, shape, cache, q, table, lens, out, lse
     return guarded([&] {
         const Call c(a, nargs, 9);
@@ -154,7 +175,7 @@ PyObject* paged_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {       
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) { return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr}; }
 PyMethodDef methods[] = {method<packed_prefill>("packed_prefill"), method<cache_write>("cache_write"), method<cache_read>("cache_read"),
-                         method<paged_attend>("paged_attend"), {nullptr, nullptr, 0, nullptr}};
+                         method<norm_rotate>("norm_rotate"), method<paged_attend>("paged_attend"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lspages", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -1,0 +1,201 @@
+// Norms of queries and keys head by head, and the rotation by their positions, in one pass (ls_norm_rotate):
+//     y = x / sqrt(mean(x^2) + eps) * w,     (a, b) -> (a cos t - b sin t, b cos t + a sin t)  for the pairs of the first `dims` values,  t = position * freq[pair],
+// into rows, and K (with V as it is) into the pages of a cache by their slots.
+//
+// Bound by memory: each row is read and written once.  A row of a head is d / 16 neighbouring lanes', eight values here and eight there: of those that are rotated the chunks of eight values c and
+// c + dims / 16, so that both values of a pair are in one lane whichever way pairs are counted, and its eight angles serve all heads of the row.
+// Angles.  A position times a frequency is formed in 64 bits and brought into a quarter turn there (t - k pi / 2 with pi / 2 in two parts): in 32 bits the angle of position 260000 would be off by up to
+// 2^-7.  Sine and cosine of what is left, at most pi / 4, are their series up to t^9 and t^10, whose next terms are below 2^-29.
+// Pages.  What a row becomes is rounded to the rows' type and then stored as ls_cache_write stores it, so that both ways give the same pages; 8 and 4 bits want
+// neighbouring values in a lane, which LDS brings together (a row's lanes are one wave's: no barrier).
+#include "ls_rows.h"
+
+namespace ls {
+
+constexpr int ROTATE_THREADS = 256;
+constexpr int NO_PAGES = -1;
+
+// Sum over the L (4 or 8) neighbouring lanes of a row, in every lane
+template <int L>
+__device__ __forceinline__ float row_sum(float x) {
+    auto with = [](float v, auto ctrl) {
+        return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    x = with(x, std::integral_constant<int, 0xB1>{});      // quad_perm 1,0,3,2
+    x = with(x, std::integral_constant<int, 0x4E>{});      // quad_perm 2,3,0,1
+    if (L == 8) x = with(x, std::integral_constant<int, 0x141>{});                           // row_half_mirror
+    return x;
+}
+
+__device__ __forceinline__ void sine_cosine(double t, float& sine, float& cosine) {
+    const double k = __builtin_rint(t * 0.63661977236758134308);               // quarter turns
+    const float x = (float)__builtin_fma(-k, 6.123233995736766036e-17, __builtin_fma(-k, 1.5707963267948965580, t));
+    const int quarter = (int)__builtin_fma(-4.0, __builtin_rint(k * 0.25), k);  // -2 .. 2
+    const float y = x * x;
+    float s = __builtin_fmaf(y, 1.f / 362880.f, -1.f / 5040.f), c = __builtin_fmaf(y, -1.f / 3628800.f, 1.f / 40320.f);
+    s = __builtin_fmaf(y, s, 1.f / 120.f);
+    c = __builtin_fmaf(y, c, -1.f / 720.f);
+    s = __builtin_fmaf(y, s, -1.f / 6.f);
+    c = __builtin_fmaf(y, c, 1.f / 24.f);
+    c = __builtin_fmaf(y, c, -0.5f);
+    s = __builtin_fmaf(y * x, s, x);
+    c = __builtin_fmaf(y, c, 1.f);
+    sine = quarter & 1 ? c : s;
+    cosine = quarter & 1 ? s : c;
+    if (quarter & 2) sine = -sine;
+    if ((quarter + 1) & 2) cosine = -cosine;
+}
+
+template <typename T, int TYPE, int D, bool NEIGHBOURS>
+__global__ __launch_bounds__(ROTATE_THREADS) void rotate_kernel(RotateArgs a) {
+    constexpr int L = D / 16, GROUPS = ROTATE_THREADS / L, SIZE = Elem<T>::bytes;
+    constexpr bool GATHER = TYPE == CACHE_E4M3 || TYPE == CACHE_E2M1;
+    __shared__ __align__(16) unsigned char rows_s[GATHER ? GROUPS * D * SIZE : 16];
+    const int group = threadIdx.x / L, p = threadIdx.x % L;
+    const int64_t item = (a.group0 + blockIdx.x) * GROUPS + group;
+    const int64_t row = item / a.splits;
+    if (row >= (int64_t)a.B * a.n_hat) return;
+    const int b = (int)(row / a.n_hat), i = (int)(row - (int64_t)b * a.n_hat);
+    // ---- what this lane has of a row, its angles, and where in the pages the row goes
+    const int turned = a.dims / 16;
+    const bool turns = p < turned;
+    const int c0 = turns ? p : 2 * p, c1 = turns ? p + turned : 2 * p + 1;
+    auto address = [&](const RowArgs& r, int h) { return r.data + ((int64_t)b * r.seq + (int64_t)i * r.row + (int64_t)h * r.head) * SIZE; };
+    Eight<T> x[2], next[2];
+    auto load = [&](int h, Eight<T> (&to)[2]) {
+        const bool is_v = TYPE != NO_PAGES && h >= a.Hq + a.Hkv;
+        const unsigned char* r = h < a.Hq ? address(a.q, h) : is_v ? address(a.v, h - a.Hq - a.Hkv) : address(a.k, h - a.Hq);
+        to[0].load(r + (is_v ? 2 * p : c0) * (8 * SIZE));
+        to[1].load(r + (is_v ? 2 * p + 1 : c1) * (8 * SIZE));
+    };
+    int h = (int)(item - row * a.splits);
+    load(h, x);
+    const int position = a.positions ? a.positions[row] : i;
+    int page = -1, place = 0;
+    if constexpr (TYPE != NO_PAGES) {
+        const int64_t slot = a.slots[row], at = slot >> a.cache.page_log;
+        if (slot >= 0 && at < (int64_t)a.cache.pages) { page = (int)at; place = (int)(slot & ((1 << a.cache.page_log) - 1)); }
+        else if (slot >= 0 && p == 0) atomicOr(a.status, STAT_PAGE_RANGE);
+    }
+    float sine[8], cosine[8];
+    if (turns) {
+        const f32x4 f0 = *reinterpret_cast<const f32x4*>(a.freq + (NEIGHBOURS ? 4 * c0 : 8 * p)), f1 = *reinterpret_cast<const f32x4*>(a.freq + (NEIGHBOURS ? 4 * c1 : 8 * p + 4));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sine_cosine((double)position * (double)(e < 4 ? f0[e & 3] : f1[e & 3]), sine[e], cosine[e]);
+    }
+    int weighs = 0;                                        // whose weights are at hand: 1 the queries', 2 the keys'
+    f32x4 w[4];
+    for (; h < a.heads; h += a.splits) {
+        const bool more = h + a.splits < a.heads;
+        if (more) load(h + a.splits, next);
+        const bool is_q = h < a.Hq;
+        if (TYPE == NO_PAGES || h < a.Hq + a.Hkv) {
+            float y[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = x[e / 8].at(e % 8);
+            const float* weight = is_q ? a.q_weight : a.k_weight;
+            if (weight) {
+                if (weighs != (is_q ? 1 : 2)) {
+                    weighs = is_q ? 1 : 2;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = *reinterpret_cast<const f32x4*>(weight + 8 * (e < 2 ? c0 : c1) + 4 * (e & 1));
+                }
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum = __builtin_fmaf(y[e], y[e], sum);
+                sum = row_sum<L>(sum);
+                if (sum < 0x1p100f && (sum > 0x1p-60f || a.eps > 0x1p-40f)) {
+                    const float f = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.f / D, a.eps));
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[e] = y[e] * f * w[e / 4][e % 4];
+                } else {                                   // squares that fp32 cannot hold
+                    double s = 0.0;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s = __builtin_fma((double)y[e], (double)y[e], s);
+#pragma unroll
+                    for (int o = 1; o < L; o *= 2) s += __shfl_xor(s, o, 64);
+                    const double f = 1.0 / sqrt(s * (1.0 / D) + (double)a.eps);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[e] = (float)((double)y[e] * f * (double)w[e / 4][e % 4]);
+                }
+            }
+            if (turns) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {              // angle e's pair
+                    const int u = NEIGHBOURS ? 8 * (e / 4) + 2 * (e % 4) : e, v = NEIGHBOURS ? u + 1 : e + 8;
+                    const float z = __builtin_fmaf(y[u], cosine[e], -(y[v] * sine[e]));
+                    y[v] = __builtin_fmaf(y[v], cosine[e], y[u] * sine[e]);
+                    y[u] = z;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) x[e / 8].set(e % 8, y[e]);
+            if (is_q || a.k_out.data) {
+                unsigned char* r = is_q ? address(a.q_out, h) : address(a.k_out, h - a.Hq);
+                x[0].store(r + c0 * (8 * SIZE));
+                x[1].store(r + c1 * (8 * SIZE));
+            }
+        }
+        if constexpr (TYPE != NO_PAGES) {
+            if (!is_q && page >= 0) {
+                const bool is_v = h >= a.Hq + a.Hkv;
+                const int j = h - a.Hq - (is_v ? a.Hkv : 0);
+                const int64_t r = (((int64_t)page * a.cache.Hkv + j) << a.cache.page_log) + place;
+                unsigned char* pool = is_v ? a.cache.v : a.cache.k;
+                uint8_t* exps = is_v ? a.cache.vx : a.cache.kx;
+                if constexpr (GATHER) {
+                    if (!is_v) {
+                        unsigned char* mine = rows_s + group * D * SIZE;
+                        __builtin_amdgcn_wave_barrier();   // (the reads of the head before come first)
+                        x[0].store(mine + c0 * (8 * SIZE));
+                        x[1].store(mine + c1 * (8 * SIZE));
+                        __builtin_amdgcn_wave_barrier();
+                        x[0].load(mine + 2 * p * (8 * SIZE));
+                        x[1].load(mine + (2 * p + 1) * (8 * SIZE));
+                    }
+                    store_part<TYPE, D, 16>(x, pool, exps, r, p);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        Eight<bf16_t> z;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z.set(e, x[c].at(e));
+                        z.store(pool + r * (2 * D) + (is_v ? 2 * p + c : c ? c1 : c0) * 16);
+                    }
+                }
+            }
+        }
+        if (more) { x[0] = next[0]; x[1] = next[1]; }
+    }
+}
+
+template <typename T, int TYPE, int D>
+static hipError_t run_rotate_t(RotateArgs a, hipStream_t st) {
+    constexpr int GROUPS = ROTATE_THREADS / (D / 16), WAVE = 64 / (D / 16);
+    const int64_t rows = (int64_t)a.B * a.n_hat;
+    a.heads = a.Hq + (TYPE == NO_PAGES ? 1 : 2) * a.Hkv;
+    // A wave a row, whose groups of lanes take its heads in turn; of few rows each group has a head.
+    a.splits = rows * a.heads <= 2048 * WAVE || a.heads < WAVE ? a.heads : WAVE;
+    const int64_t blocks = (rows * a.splits + GROUPS - 1) / GROUPS;
+    for (a.group0 = 0; a.group0 < blocks; a.group0 += MOVE_GROUPS) {
+        const int64_t here = blocks - a.group0 < MOVE_GROUPS ? blocks - a.group0 : MOVE_GROUPS;
+        if (a.neighbours) hipLaunchKernelGGL((rotate_kernel<T, TYPE, D, true>), dim3((uint32_t)here), dim3(ROTATE_THREADS), 0, st, a);
+        else hipLaunchKernelGGL((rotate_kernel<T, TYPE, D, false>), dim3((uint32_t)here), dim3(ROTATE_THREADS), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+template <typename T, int TYPE>
+static hipError_t run_rotate_d(const RotateArgs& a, int d, hipStream_t st) { return d == 128 ? run_rotate_t<T, TYPE, 128>(a, st) : run_rotate_t<T, TYPE, 64>(a, st); }
+template <typename T>
+static hipError_t run_rotate_p(const RotateArgs& a, int type, int d, hipStream_t st) {
+    if (type == CACHE_E2M1) return run_rotate_d<T, CACHE_E2M1>(a, d, st);
+    if (type == CACHE_E4M3) return run_rotate_d<T, CACHE_E4M3>(a, d, st);
+    return type == CACHE_BF16 ? run_rotate_d<T, CACHE_BF16>(a, d, st) : run_rotate_d<T, NO_PAGES>(a, d, st);
+}
+hipError_t run_rotate(const RotateArgs& a, int dtype, int type, int d, hipStream_t st) {
+    return dtype == 0 ? run_rotate_p<bf16_t>(a, type, d, st) : run_rotate_p<float>(a, type, d, st);
+}
+
+}  // namespace ls

@@ -12,6 +12,9 @@
 
 namespace ls {
 
+// Workgroups of a launch.  A dimension of a grid has less than 2^32 threads: of one that has more, HIP runs what is left of the number modulo 2^32, and says nothing.
+constexpr int64_t MOVE_GROUPS = 1 << 23;
+
 constexpr int stored_bytes(int type, int d) { return type == CACHE_BF16 ? 2 * d : type == CACHE_E4M3 ? d : d / 2; }         // of a row's values
 constexpr int stored_exps(int type, int d) { return type == CACHE_BF16 ? 0 : type == CACHE_E4M3 ? 1 : d / 32; }             // and its exponents
 
