@@ -336,6 +336,32 @@ int ls_cache_read(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, con
                   const int32_t* starts, const int32_t* count, const int32_t* table, int32_t max_pages,
                   const int32_t* pos, void* hip_stream);
 
+/*
+ * ls_cache_resize -- sequences that grow and shrink: pages for them from a ring of free ones and back to it, and for the rows that a step adds what the other calls
+ * take.  Once a step, for all layers whose pools are alike (they share the table).
+ *
+ *   shape: B sequences, Hkv and d of the cache; n_hat >= 1: rows that positions and slots have room for.  Hq, n, w, dtype, scale are as elsewhere, and ignored.
+ *   cache: of which `page` and `pages` are used
+ *   free_pages [pages] int32, state [2] int32: a ring.  The numbers of the free pages are its `state[1]` entries from entry state[0] on, and behind the last entry comes
+ *        the first.  (In the beginning: 0 .. pages - 1, and {0, pages}.)
+ *   len [B] int32: positions that each sequence has; add [B] int32: by how many it grows, or, negative, shrinks (to none at least)
+ *   Sequences that grow take the pages that they have none for from the front of the ring, in order of the sequences; table entries of what they have stay.  One that asks
+ *   for more than the ring holds besides what all before it ask for does not grow (LS_STAT_PAGES_OUT), nor one that would be longer than max_pages pages or 2^31 - 1
+ *   (LS_STAT_PAGE_RANGE).  Sequences that shrink give the pages that they no longer need to the back of the ring, in order, for calls to come; their table entries stay, and mean nothing.
+ *   A length outside [0, max_pages * page] stays as it is, likewise a ring that does not have that many (it holds no page then, and pages that it has no room for are lost; LS_STAT_PAGE_RANGE).
+ *   Pages that several sequences share are each sequence's here: give them back once.
+ * Outputs (device memory; new_len and new_state may be len and state themselves):
+ *   new_len [B], new_state [2], table, free_pages
+ *   starts [B+1] int32 or NULL: the rows of the step, packed: sequence b adds rows starts[b] .. starts[b+1] - 1, add[b] of them where that is positive (also where it
+ *        does not grow).  A sequence whose rows go beyond n_hat has none and does not grow, like all behind it (LS_STAT_STARTS).
+ *   positions [n_hat] int32 or NULL: of each row, 0 where its sequence does not grow and behind the last sequence
+ *   slots [n_hat] int64 or NULL: page * (positions of a page) + place in it of each row, as ls_norm_rotate takes it; -1 there
+ * No workspace.
+ */
+int ls_cache_resize(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, int32_t* free_pages, const int32_t* state, int32_t* new_state,
+                    const int32_t* add, const int32_t* len, int32_t* new_len, int32_t* table, int32_t max_pages,
+                    int32_t* starts, int32_t* positions, int64_t* slots, void* hip_stream);
+
 /* The norms and the rotation that ls_norm_rotate gives queries and keys.  Device memory, fp32, 16-byte aligned. */
 typedef enum { LS_PAIRS_HALVES = 0, LS_PAIRS_NEIGHBOURS = 1 } ls_pairs;
 typedef struct {
@@ -412,9 +438,10 @@ int ls_profile_prefill_kernel_ms(ls_ctx* ctx, double* mean_ms, int32_t* launches
                                    head's columns were ignored (its diagonals still apply) */
 #define LS_STAT_MERGE_RANGE 32  /* ls_merge_lines: input entries outside [0, n) were dropped */
 #define LS_STAT_PAGE_RANGE  64  /* ls_cache_write, ls_cache_read, ls_norm_rotate, ls_paged_attend: a position lies in no page of the pool or beyond
-                                   the table; it was left out */
+                                   the table; it was left out.  ls_cache_resize: so would a sequence's, or its length or the ring is none */
 #define LS_STAT_STARTS     128  /* ls_packed_prefill, ls_cache_write, ls_cache_read: a sequence's starts descend or leave the rows;
-                                   it was passed by, with all behind it */
+                                   it was passed by, with all behind it.  ls_cache_resize: its rows have no room */
+#define LS_STAT_PAGES_OUT  256  /* ls_cache_resize: a sequence did not grow, for want of free pages */
 int ls_poll_status(ls_ctx* ctx, int32_t* host_out, void* hip_stream);
 
 #ifdef __cplusplus

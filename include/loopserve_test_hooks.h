@@ -80,6 +80,9 @@ int ls_debug_check_move(const ls_shape* shape, const ls_cache* cache, const ls_r
 int ls_debug_check_paged(const ls_shape* shape, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages, const int32_t* len,
                          const void* out, const float* lse);
 
+int ls_debug_check_resize(const ls_shape* shape, const ls_cache* cache, const int32_t* free_pages, const int32_t* state, const int32_t* new_state, const int32_t* add,
+                          const int32_t* len, const int32_t* new_len, const int32_t* table, int32_t max_pages, const int32_t* starts, const int32_t* positions,
+                          const int64_t* slots);
 int ls_debug_check_rotate(const ls_shape* shape, const ls_rotation* rotation, const ls_rows* q, const ls_rows* k, const int32_t* positions, const ls_rows* q_out,
                           const ls_rows* k_out, const ls_cache* cache, const ls_rows* v, const int64_t* slots);
 

@@ -25,7 +25,7 @@ ENTRY_POINTS = ("ls_workspace_bytes", "ls_create", "ls_destroy", "ls_last_error"
                 "ls_score", "ls_select", "ls_sparse_prefill", "ls_kv_compress", "ls_poll_status")
 # bits of the device status word (ls_poll_status)
 LS_STAT_WALK_TIMEOUT, LS_STAT_S_TRUNCATED, LS_STAT_V_TRUNCATED, LS_STAT_S_RANGE, LS_STAT_V_INVALID = 1, 2, 4, 8, 16
-LS_STAT_MERGE_RANGE, LS_STAT_PAGE_RANGE, LS_STAT_STARTS = 32, 64, 128
+LS_STAT_MERGE_RANGE, LS_STAT_PAGE_RANGE, LS_STAT_STARTS, LS_STAT_PAGES_OUT = 32, 64, 128, 256
 LS_CACHE_BF16, LS_CACHE_E4M3, LS_CACHE_E2M1 = 0, 1, 4
 LS_PAIRS_HALVES, LS_PAIRS_NEIGHBOURS = 0, 1
 
@@ -114,6 +114,10 @@ def load_library():
     tp = C.POINTER(LsRotation)
     lib.ls_norm_rotate.restype = C.c_int
     lib.ls_norm_rotate.argtypes = [vp, sp, tp, rp, rp, vp, rp, rp, cp, rp, vp, vp]
+    lib.ls_cache_resize.restype = C.c_int
+    lib.ls_cache_resize.argtypes = [vp, sp, cp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+    lib.ls_debug_check_resize.restype = C.c_int
+    lib.ls_debug_check_resize.argtypes = [sp, cp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp]
     lib.ls_debug_check_rotate.restype = C.c_int
     lib.ls_debug_check_rotate.argtypes = [sp, tp, rp, rp, vp, rp, rp, cp, rp, vp]
     lib.ls_debug_page_of.restype = C.c_int
@@ -355,6 +359,13 @@ class Context:
         if rc:
             self._check(rc)
 
+    def ls_cache_resize(self, shape, cache, free, state, add, lens, table, new_state=None, new_lens=None, starts=None, positions=None, slots=None):
+        """free, state, lens and table as alloc_pages makes them.  new_state, new_lens None: state and lens are updated."""
+        rc = self.pages.cache_resize(self.hv, self.device, shape, self._pages(cache), free, state, state if new_state is None else new_state, add, lens,
+                                     lens if new_lens is None else new_lens, table, starts, positions, slots)
+        if rc:
+            self._check(rc)
+
     def ls_norm_rotate(self, shape, rotation, q, k, q_out, k_out=None, positions=None, cache=None, v=None, slots=None):
         """k_out None: keys go into the cache only.  cache, v, slots together, or none of them."""
         if rotation.device not in (None, self.device):
@@ -468,6 +479,13 @@ def alloc_select(shape: LsShape, cap_v=None, cap_s=None, device="cuda", accounte
     return dict(v_idx=torch.empty(B, Hq, cap_v or n, **i), v_cnt=torch.empty(B, Hq, **i),
                 s_idx=torch.empty(B, Hq, cap_s or n, **i), s_cnt=torch.empty(B, Hq, **i),
                 accounted=torch.empty(B, Hq, dtype=torch.float32, device=device) if accounted else None)
+
+
+def alloc_pages(cache: PagedCache, B: int, max_pages: int):
+    """What ls_cache_resize keeps for B sequences without a position: the ring of free pages, all of the cache's, lengths and block table."""
+    i = dict(dtype=torch.int32, device=cache.k.device)
+    pages = cache.k.shape[0]
+    return dict(free=torch.arange(pages, **i), state=torch.tensor([0, pages], **i), lens=torch.zeros(B, **i), table=torch.full((B, max_pages), -1, **i))
 
 
 def default_scale(d):

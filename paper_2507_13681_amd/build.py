@@ -11,7 +11,7 @@ LIB = os.path.join(_DIR, "libloopserve.so")
 NATIVE = os.path.join(_DIR, "_lsnative.so")
 PAGES = os.path.join(_DIR, "_lspages.so")
 SOURCES = ["ls_api.hip", "ls_score.hip", "ls_select.hip", "ls_prefill.hip", "ls_decode.hip", "ls_cache.hip",
-           "ls_paged.hip", "ls_paged4.hip", "ls_rotate.hip", "ls_packed.hip"]
+           "ls_paged.hip", "ls_paged4.hip", "ls_rotate.hip", "ls_resize.hip", "ls_packed.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-ffp-contract=off",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Wno-inline-asm"]

@@ -18,7 +18,7 @@ static_assert(ls::TOPB_MAX_LEN == LS_MAX_N, "ls_kv_compress documents LS_MAX_N a
 static_assert(ls::STAT_WALK_TIMEOUT == LS_STAT_WALK_TIMEOUT && ls::STAT_S_TRUNCATED == LS_STAT_S_TRUNCATED &&
               ls::STAT_V_TRUNCATED == LS_STAT_V_TRUNCATED && ls::STAT_S_RANGE == LS_STAT_S_RANGE &&
               ls::STAT_V_INVALID == LS_STAT_V_INVALID && ls::STAT_MERGE_RANGE == LS_STAT_MERGE_RANGE &&
-              ls::STAT_PAGE_RANGE == LS_STAT_PAGE_RANGE && ls::STAT_STARTS == LS_STAT_STARTS,
+              ls::STAT_PAGE_RANGE == LS_STAT_PAGE_RANGE && ls::STAT_STARTS == LS_STAT_STARTS && ls::STAT_PAGES_OUT == LS_STAT_PAGES_OUT,
               "status bits of the kernels and of the header");
 static_assert(ls::CACHE_BF16 == LS_CACHE_BF16 && ls::CACHE_E4M3 == LS_CACHE_E4M3 && ls::CACHE_E2M1 == LS_CACHE_E2M1, "types of pages of the kernels and of the header");
 
@@ -731,6 +731,22 @@ int cache_move(ls_ctx* c, const char* who, bool write, const ls_shape* s, const 
     return LS_OK;
 }
 
+// Whether two arrays of n words share some but do not begin together
+bool overlap(const int32_t* a, const int32_t* b, int64_t n) { return a != b && a < b + n && b < a + n; }
+Wrong check_resize(const ls_shape* s, const ls_cache* cache, const int32_t* free_pages, const int32_t* state, const int32_t* new_state, const int32_t* add,
+                   const int32_t* len, const int32_t* new_len, const int32_t* table, int32_t max_pages, const int32_t* starts, const int32_t* positions, const int64_t* slots) {
+    Wrong w = check_heads(s, false);
+    if (w.code) return w;
+    if (s->n_hat < 1 || s->n_hat > MOST_ROWS) return {LS_ESHAPE, "rows out of range"};
+    if ((w = check_cache(cache, s, table, max_pages)).code) return w;
+    if (!free_pages || !state || !new_state || !add || !len || !new_len) return {LS_EINVAL, "NULL tensor"};
+    for (const int32_t* p : {free_pages, state, new_state, add, len, new_len, table, starts, positions})
+        if (!aligned4(p)) return {LS_EINVAL, "misaligned index tensor"};
+    if (reinterpret_cast<uintptr_t>(slots) & 7u) return {LS_EINVAL, "misaligned index tensor"};
+    if (overlap(state, new_state, 2) || overlap(len, new_len, s->B)) return {LS_EINVAL, "an output overlaps its input without being it"};
+    return FINE;
+}
+
 Wrong check_rotate(const ls_shape* s, const ls_rotation* r, const ls_rows* q, const ls_rows* k, const int32_t* positions, const ls_rows* q_out, const ls_rows* k_out,
                    const ls_cache* cache, const ls_rows* v, const int64_t* slots) {
     Wrong w = check_heads(s, true);
@@ -806,6 +822,23 @@ int ls_cache_write(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const ls
 int ls_cache_read(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const ls_rows* k, const ls_rows* v, const int32_t* starts,
                   const int32_t* count, const int32_t* table, int32_t max_pages, const int32_t* pos, void* stream) {
     return cache_move(c, "ls_cache_read", false, s, cache, k, v, starts, count, table, max_pages, pos, stream);
+}
+
+int ls_cache_resize(ls_ctx* c, const ls_shape* s, const ls_cache* cache, int32_t* free_pages, const int32_t* state, int32_t* new_state, const int32_t* add,
+                    const int32_t* len, int32_t* new_len, int32_t* table, int32_t max_pages, int32_t* starts, int32_t* positions, int64_t* slots, void* stream) {
+    if (!c) return LS_EINVAL;
+    if (const Wrong w = check_resize(s, cache, free_pages, state, new_state, add, len, new_len, table, max_pages, starts, positions, slots); w.code)
+        return fail(c, w.code, "ls_cache_resize: %s", w.what);
+    ls::ResizeArgs a{};
+    a.free = free_pages; a.state = state; a.new_state = new_state; a.add = add; a.len = len; a.new_len = new_len; a.table = table;
+    a.starts = starts; a.positions = positions; a.slots = slots;
+    a.B = s->B; a.pages = (int)cache->pages; a.page_log = __builtin_ctz((unsigned)cache->page); a.max_pages = max_pages; a.n_rows = (int)s->n_hat;
+    a.status = c->status;
+    const OnDevice on(c->device);
+    if (!on.ok) return fail(c, LS_EHIP, "ls_cache_resize: hipSetDevice failed");
+    const hipError_t e = ls::run_resize(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail(c, LS_EHIP, "ls_cache_resize: %s", hipGetErrorString(e));
+    return LS_OK;
 }
 
 int ls_norm_rotate(ls_ctx* c, const ls_shape* s, const ls_rotation* r, const ls_rows* q, const ls_rows* k, const int32_t* positions,
@@ -1046,6 +1079,10 @@ int ls_debug_check_move(const ls_shape* s, const ls_cache* cache, const ls_rows*
 int ls_debug_check_paged(const ls_shape* s, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages, const int32_t* len,
                          const void* out, const float* lse) {
     return check_paged(s, cache, q, table, max_pages, len, out, lse).code;
+}
+int ls_debug_check_resize(const ls_shape* s, const ls_cache* cache, const int32_t* free_pages, const int32_t* state, const int32_t* new_state, const int32_t* add,
+                          const int32_t* len, const int32_t* new_len, const int32_t* table, int32_t max_pages, const int32_t* starts, const int32_t* positions, const int64_t* slots) {
+    return check_resize(s, cache, free_pages, state, new_state, add, len, new_len, table, max_pages, starts, positions, slots).code;
 }
 int ls_debug_check_rotate(const ls_shape* s, const ls_rotation* r, const ls_rows* q, const ls_rows* k, const int32_t* positions, const ls_rows* q_out,
                           const ls_rows* k_out, const ls_cache* cache, const ls_rows* v, const int64_t* slots) {

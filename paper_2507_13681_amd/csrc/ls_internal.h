@@ -219,6 +219,15 @@ struct RotateArgs {
     int32_t* status;
 };
 
+struct ResizeArgs {
+    int32_t *free, *new_state, *new_len, *table, *starts, *positions;
+    int64_t* slots;
+    const int32_t *state, *add, *len;
+    int B, pages, page_log, max_pages, n_rows;
+    int bulk, finish;         // what a launch does: pages and rows; lengths, starts and the ring's state
+    int32_t* status;
+};
+
 // ls_paged_attend.  A unit of work is a part of the 32-key tiles of one KV head of one sequence, and a workgroup has one.  Which one follows from the lengths, which only the device
 // knows.
 constexpr int PAGED_TILE = 32;               // keys
@@ -339,7 +348,7 @@ struct PackedArgs {
 
 // status bits (mirrors of LS_STAT_* in loopserve.h)
 constexpr int STAT_WALK_TIMEOUT = 1, STAT_S_TRUNCATED = 2, STAT_V_TRUNCATED = 4, STAT_S_RANGE = 8, STAT_V_INVALID = 16,
-              STAT_MERGE_RANGE = 32, STAT_PAGE_RANGE = 64, STAT_STARTS = 128;
+              STAT_MERGE_RANGE = 32, STAT_PAGE_RANGE = 64, STAT_STARTS = 128, STAT_PAGES_OUT = 256;
 constexpr int WALK_SPIN_DEFAULT = 1 << 22;   // never reached in practice (about a second of polling)
 
 // Lets a kernel use all of a compute unit's LDS (160 KB, less what the kernel declares statically) as
@@ -366,6 +375,7 @@ hipError_t run_packed(const PackedArgs& a, int dtype, int d, hipStream_t st);
 PackedCut packed_cut(int B, bool packed, int64_t keys, int64_t queries, int Hkv, int G, int dtype, int d, int64_t room);           // with room for so many parts' results
 int64_t packed_items(int B, int64_t n_hat, int Hkv, int G, bool packed);       // no fewer than there are
 hipError_t run_move(const MoveArgs& a, bool write, int dtype, int type, int d, hipStream_t st);
+hipError_t run_resize(ResizeArgs a, hipStream_t st);
 hipError_t run_rotate(const RotateArgs& a, int dtype, int type, int d, hipStream_t st);         // type -1: no pages
 hipError_t run_paged(const PagedArgs& a, int type, int d, int units, hipStream_t st);
 hipError_t init_paged4_kernels();

@@ -136,6 +136,21 @@ PyObject* move(PyObject* const* a, Py_ssize_t nargs, F call) {                  
 }
 PyObject* cache_write(PyObject*, PyObject* const* a, Py_ssize_t nargs) { return move(a, nargs, ls_cache_write); }
 PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t nargs) { return move(a, nargs, ls_cache_read); }
+PyObject* cache_resize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {          // ctx, device, shape, cache, free, state, new_state, add, len, new_len, table, starts, positions, slots
+    return guarded([&] {
+        const Call c(a, nargs, 14);
+        const ls_shape& s = c.sh;
+        const ls_cache cache = struct_of<ls_cache>(a[3], "LsCache");
+        auto words = [&](int i, const char* name, int64_t n) { return static_cast<int32_t*>(plain(a[i], name, I32, c.device, {n})); };
+        int32_t* free_pages = words(4, "free", cache.pages);
+        int32_t *state = words(5, "state", 2), *new_state = words(6, "new_state", 2), *add = words(7, "add", s.B), *len = words(8, "lens", s.B), *new_len = words(9, "new_lens", s.B);
+        int32_t max_pages = 0;
+        int32_t* table = static_cast<int32_t*>(plain(a[10], "table", I32, c.device, {s.B, -1}, &max_pages));
+        int32_t *starts = words(11, "starts", (int64_t)s.B + 1), *positions = words(12, "positions", s.n_hat);
+        int64_t* slots = static_cast<int64_t*>(plain(a[13], "slots", at::kLong, c.device, {s.n_hat}));
+        return released([&] { return ls_cache_resize(c.ctx, &s, &cache, free_pages, state, new_state, add, len, new_len, table, max_pages, starts, positions, slots, c.stream); });
+    });
+}
 PyObject* norm_rotate(PyObject*, PyObject* const* a, Py_ssize_t nargs) {           // ctx, device, shape, rotation, q, k, q_out, k_out, positions, cache, v, slots
     return guarded([&] {
         Call c(a, nargs, 12);
@@ -175,7 +190,7 @@ PyObject* paged_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {       
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) { return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr}; }
 PyMethodDef methods[] = {method<packed_prefill>("packed_prefill"), method<cache_write>("cache_write"), method<cache_read>("cache_read"),
-                         method<norm_rotate>("norm_rotate"), method<paged_attend>("paged_attend"), {nullptr, nullptr, 0, nullptr}};
+                         method<cache_resize>("cache_resize"), method<norm_rotate>("norm_rotate"), method<paged_attend>("paged_attend"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lspages", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
