@@ -29,7 +29,21 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
     const int64_t row0 = (a.group0 + blockIdx.x) * ROWS;
     const bool first = row0 == 0 && blockIdx.y == 0;
     int b = -1, i = 0;
-    int64_t at = row0 + slot;                              // the row, and that of the tensor it is
+    int64_t at = row0 + slot, seq = 0;                     // the row, and that of the tensor it is
+    const bool is = at < (a.starts ? 1 : (int64_t)a.B) * a.n_hat;
+    if (!a.starts) {
+        seq = is ? at / a.n_hat : 0;
+        at -= seq * a.n_hat;
+    }
+    const int h0 = blockIdx.y * a.heads, h1 = h0 + a.heads < a.cache.Hkv ? h0 + a.heads : a.cache.Hkv;
+    unsigned char* const rows[2] = {a.k.data + (seq * a.k.seq + at * a.k.row + 8 * part) * SRC, a.v.data + (seq * a.v.seq + at * a.v.row + 8 * part) * SRC};
+    const int64_t step[2] = {a.k.head * SRC, a.v.head * SRC};
+    Eight<T> ahead[4];                                     // rows that are written are asked for before it is known where they go
+    auto ask = [&](int h) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ahead[j].load(rows[j & 1] + (h + j / 2) * step[j & 1]);
+    };
+    if (WRITE && is && h0 + 2 <= h1) ask(h0);
     if (a.starts) {
         // Each sequence lays claim to its rows among these, up to the first one whose starts are none.
         if (tid < ROWS) seq_s[tid] = -1;
@@ -48,10 +62,9 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
         __syncthreads();
         b = seq_s[slot];
         if (b >= 0) i = (int)(at - a.starts[b]);
-    } else if (at < (int64_t)a.B * a.n_hat) {
-        b = (int)(at / a.n_hat);
-        i = (int)(at - (int64_t)b * a.n_hat);
-        at = i;
+    } else if (is) {
+        b = (int)seq;
+        i = (int)at;
         if (a.count && i >= a.count[b]) b = -1;
     }
     int page = -1;
@@ -62,11 +75,7 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
         if (page < 0 && part == 0 && blockIdx.y == 0) atomicOr(a.status, STAT_PAGE_RANGE);
     }
     if (page < 0) return;
-    const int h0 = blockIdx.y * a.heads, h1 = h0 + a.heads < a.cache.Hkv ? h0 + a.heads : a.cache.Hkv;
-    const int64_t seq = a.starts ? 0 : b;
     const int64_t place = ((int64_t)page * a.cache.Hkv << a.cache.page_log) + (p & ((1 << a.cache.page_log) - 1));       // of head 0, in rows
-    unsigned char* const rows[2] = {a.k.data + (seq * a.k.seq + at * a.k.row + 8 * part) * SRC, a.v.data + (seq * a.v.seq + at * a.v.row + 8 * part) * SRC};
-    const int64_t step[2] = {a.k.head * SRC, a.v.head * SRC};
     unsigned char* const pool[2] = {a.cache.k, a.cache.v};
     uint8_t* const exps[2] = {a.cache.kx, a.cache.vx};
     auto put = [&](const Eight<T>& x, int h, int t) {      // into the cache
@@ -76,11 +85,9 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
     if constexpr (WRITE) {
         int h = h0;
         for (; h + 2 <= h1; h += 2) {                      // four rows in flight
-            Eight<T> x[4];
+            if (h != h0) ask(h);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j].load(rows[j & 1] + (h + j / 2) * step[j & 1]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) put(x[j], h + j / 2, j & 1);
+            for (int j = 0; j < 4; ++j) put(ahead[j], h + j / 2, j & 1);
         }
         for (; h < h1; ++h)
 #pragma unroll
