@@ -895,13 +895,14 @@ int ls_paged_attend(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const v
     a.cache = cache_args(cache, table, max_pages);
     a.q = q; a.len = len; a.out = out; a.lse = lse; a.part = reinterpret_cast<float*>(c->ws);
     a.B = s->B; a.Hq = s->Hq; a.Hkv = s->Hkv; a.G = s->Hq / s->Hkv; a.most = s->n; a.scale_log2e = scale_log2e(s); a.status = c->status;
-    const bool joins = ls::paged_joins(s->B, s->Hkv, a.G, s->n), counts = joins && ls::paged_most_cuts(s->B, s->Hkv, s->n) > 1;
+    a.whole = ls::paged_whole(cache->type, (int64_t)s->B * s->Hkv);
+    const bool joins = ls::paged_joins(s->B, s->Hkv, a.G, s->n, a.whole), counts = joins && ls::paged_most_cuts(s->B, s->Hkv, s->n, a.whole) > 1;
     a.done = joins ? decode_set(c, c->decode_calls) : nullptr;
     a.done_clear = decode_set(c, c->decode_calls + 2);
     a.clear_heads = !counts ? 0 : c->decode_heads > s->B * s->Hkv ? c->decode_heads : s->B * s->Hkv;
     const OnDevice on(c->device);
     if (!on.ok) return fail(c, LS_EHIP, "ls_paged_attend: hipSetDevice failed");
-    const hipError_t e = ls::run_paged(a, cache->type, s->d, ls::paged_units(s->B, s->Hkv, s->n), static_cast<hipStream_t>(stream));
+    const hipError_t e = ls::run_paged(a, cache->type, s->d, ls::paged_units(s->B, s->Hkv, s->n, a.whole), static_cast<hipStream_t>(stream));
     if (counts) { ++c->decode_calls; c->decode_heads = a.clear_heads; }
     if (e != hipSuccess) return fail(c, LS_EHIP, "ls_paged_attend: %s", hipGetErrorString(e));
     return LS_OK;

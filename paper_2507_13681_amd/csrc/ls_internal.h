@@ -240,7 +240,14 @@ __host__ __device__ inline bool paged_at_once(int64_t heads) { return heads * 4 
 // Tiles that a head is not cut for, two a wave.  Whole / in parts, us: 32 tiles 14.3 / 8.9, 17 tiles 9.8 / 8.7, 10 tiles 7.1 / 8.3, 16 tiles of 32 sequences 10.6 / 14.0
 constexpr int PAGED_WHOLE = 16;
 constexpr int PAGED_SHORTEST = 4, PAGED_SHORTEST_MANY = 32;                          // tiles of a part at least; of that many heads
-__host__ __device__ inline int paged_cuts(int tiles, int length) { return tiles <= PAGED_WHOLE ? 1 : (int)(((uint32_t)tiles + (uint32_t)length - 1) / (uint32_t)length); }
+// .. of e2m1 pages, whose tiles are read sooner, and more of many heads, which fill the chip whole.  Whole / in parts, us, sequences of 8 KV heads: 16 of 1000 11.0 / 12.5, of 2040 16.8 / 15.3, 20 of 1800
+// 15.6 / 16.1, 32 of them 16.0 / 19.4, 48 of 2040 26.3 / 27.1; 4 of 1500 13.6 / 9.9
+constexpr int PAGED_MANY_4 = 128, PAGED_WHOLE_4 = 64;
+__host__ __device__ inline int paged_whole(int type, int64_t heads) {
+    if (type != CACHE_E2M1 || heads < PAGED_MANY_4) return PAGED_WHOLE;
+    return heads * 2 / 5 < PAGED_WHOLE_4 ? (int)(heads * 2 / 5) : PAGED_WHOLE_4;
+}
+__host__ __device__ inline int paged_cuts(int tiles, int length, int whole = PAGED_WHOLE) { return tiles <= whole ? 1 : (int)(((uint32_t)tiles + (uint32_t)length - 1) / (uint32_t)length); }
 // Tiles of a part of a call, of so many tiles in all: what `length` makes of them is counted until it is accepted, four times at most, and then `enough` is taken.  (24 ragged caches of 3212 tiles: 51, 57, 60
 // and 63 tiles are too many parts, 65 would do, 81 are taken.)
 struct PagedLength {
@@ -277,6 +284,7 @@ struct PagedArgs {
     int B, Hq, Hkv, G;
     int64_t most;             // no sequence is longer
     float scale_log2e;
+    int whole;                // tiles that a head is not cut for
     int32_t* status;
 };
 
@@ -381,9 +389,9 @@ hipError_t run_paged(const PagedArgs& a, int type, int d, int units, hipStream_t
 hipError_t init_paged4_kernels();
 hipError_t run_paged4(const PagedArgs& a, int d, int units, hipStream_t st);                 // run_paged of e2m1 pages
 void launch_paged_join(const PagedArgs& a, int d, hipStream_t st);
-int paged_units(int B, int Hkv, int64_t most);                       // workgroups that sequences of up to so many keys take
-bool paged_joins(int B, int Hkv, int G, int64_t most);                      // the kernel puts parts together itself
-int paged_most_cuts(int B, int Hkv, int64_t most);                   // ... and parts of a head
+int paged_units(int B, int Hkv, int64_t most, int whole = PAGED_WHOLE);                       // workgroups that sequences of up to so many keys take
+bool paged_joins(int B, int Hkv, int G, int64_t most, int whole);                      // the kernel puts parts together itself
+int paged_most_cuts(int B, int Hkv, int64_t most, int whole = PAGED_WHOLE);                   // ... and parts of a head
 hipError_t run_score(const ScoreArgs& a, int dtype, int d, int mode, hipStream_t st);
 hipError_t run_decode(const DecodeArgs& a, int d, hipStream_t st);
 size_t decode_smem_bytes(int d, int G, int nsplit);

@@ -65,7 +65,7 @@ struct PagedUnits {
     }
     // f(lane of the sequence in order, parts, units up to and with it, lane of it): called for 64 sequences after the other until it returns true
     template <typename F>
-    __device__ bool walk(const PagedArgs& a, int lane, F f) {
+    __device__ bool walk(const PagedArgs& a, int lane, int whole, F f) {
         const int64_t room = (int64_t)a.cache.max_pages << a.cache.page_log;
         most = a.most < room ? a.most : room;
         int x = length_of(a, lane);
@@ -81,7 +81,7 @@ struct PagedUnits {
             int c, upto;
             do {
                 c = lane < here ? 1 : 0;
-                if (__ballot(t > PAGED_WHOLE) != 0ull && lane < here) c = paged_cuts(t, l.length);
+                if (__ballot(t > whole) != 0ull && lane < here) c = paged_cuts(t, l.length, whole);
                 upto = before + (int)lanes_upto((uint32_t)(c * a.Hkv));
             } while (!l.accepts(__builtin_amdgcn_readlane(upto, 63)));
             int lane_in = lane;
@@ -101,9 +101,9 @@ struct PagedUnits {
         }
         return false;
     }
-    __device__ bool find(const PagedArgs& a, int unit, int lane) {
+    __device__ bool find(const PagedArgs& a, int unit, int lane, int whole) {
         auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-        return walk(a, lane, [&](int b0, int x, int c, int l, int upto) {
+        return walk(a, lane, whole, [&](int b0, int x, int c, int l, int upto) {
             const uint64_t in = __ballot(unit < upto);
             if (in == 0ull) return false;
             const int at = __builtin_ctzll(in);
@@ -118,8 +118,8 @@ struct PagedUnits {
             return true;
         });
     }
-    __device__ bool find_head(const PagedArgs& a, int seq, int head, int lane) {       // the parts of one KV head
-        return walk(a, lane, [&](int b0, int x, int c, int l, int upto) {
+    __device__ bool find_head(const PagedArgs& a, int seq, int head, int lane, int whole) {       // the parts of one KV head
+        return walk(a, lane, whole, [&](int b0, int x, int c, int l, int upto) {
             const uint64_t in = __ballot(b0 + l == seq);
             if (in == 0ull || seq < b0 || seq >= b0 + 64) return false;
             const int at = __builtin_ctzll(in);
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
 
     // ---- which part of which head this workgroup has
     PagedUnits w;
-    if (!w.find(a, (int)blockIdx.x, lane)) return;             // (all waves of the workgroup alike)
+    if (!w.find(a, (int)blockIdx.x, lane, E2M1 ? a.whole : PAGED_WHOLE)) return;             // (all waves of the workgroup alike)
     const int b = w.b, kvh = w.kvh, cut = w.cut, cuts = w.cuts, n = w.n;
     const int bk = b * a.Hkv + kvh;
     if (cut == 0 && kvh == 0 && tid == 0 && a.len[b] > w.most) atomicOr(a.status, STAT_PAGE_RANGE);
@@ -480,7 +480,7 @@ static size_t paged_smem_t(int G, int cuts, bool joins) {
 }
 template <int D, int NH, int TYPE>
 static hipError_t run_paged_t(const PagedArgs& a, int units, hipStream_t st) {
-    size_t smem = paged_smem_t<D, NH, TYPE>(a.G, paged_most_cuts(a.B, a.Hkv, a.most), a.done != nullptr);
+    size_t smem = paged_smem_t<D, NH, TYPE>(a.G, paged_most_cuts(a.B, a.Hkv, a.most, a.whole), a.done != nullptr);
     if (a.B * a.Hkv <= PAGED_ALONE && smem <= 80 * 1024) smem = 80 * 1024 + 256;     // (a workgroup a compute unit, and none with two while another has none)
     hipLaunchKernelGGL((paged_kernel<D, NH, TYPE>), dim3(units), dim3(PG_THREADS), smem, st, a);
     if (!a.done) launch_paged_join(a, D, st);

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(2 * D) void paged_join_kernel(PagedArgs a) {
     const int tid = threadIdx.x, sub = tid / LANES, dd = 2 * (tid % LANES);
     const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, kvh = hq / a.G;
     PagedUnits w;
-    if (!w.find_head(a, b, kvh, tid & 63) || w.cuts == 1) return;
+    if (!w.find_head(a, b, kvh, tid & 63, a.whole) || w.cuts == 1) return;
     const float* src = a.part + ((int64_t)w.base * a.G + hq % a.G) * PS;
     const int64_t step = (int64_t)a.G * PS;
     float m = -INFINITY, o0 = 0.f, o1 = 0.f, l = 0.f;
@@ -73,18 +73,18 @@ void launch_paged_join(const PagedArgs& a, int d, hipStream_t st) {
 }
 
 // A head's tiles are at most all there are, and a part no shorter than these by the slots: t / paged_length(..) <= slots / Hkv, whatever t is.
-int paged_most_cuts(int B, int Hkv, int64_t most) {
+int paged_most_cuts(int B, int Hkv, int64_t most, int whole) {
     const int64_t heads = (int64_t)B * Hkv, tiles = (most + PAGED_TILE - 1) / PAGED_TILE, by_work = (paged_slots(heads) + Hkv - 1) / Hkv;
-    const int64_t by_tiles = paged_cuts((int)tiles, paged_at_once(heads) ? PAGED_SHORTEST : PAGED_SHORTEST_MANY);
+    const int64_t by_tiles = paged_cuts((int)tiles, paged_at_once(heads) ? PAGED_SHORTEST : PAGED_SHORTEST_MANY, whole);
     return (int)(by_work < by_tiles ? by_work : by_tiles);
 }
-int paged_units(int B, int Hkv, int64_t most) {
+int paged_units(int B, int Hkv, int64_t most, int whole) {
     // no more than the slots, or beside those the head that each part begins; and no more than all heads of the longest would be
-    const int64_t heads = (int64_t)B * Hkv, full = heads * paged_most_cuts(B, Hkv, most), slots = paged_slots(heads) + (paged_at_once(heads) ? 0 : heads);
+    const int64_t heads = (int64_t)B * Hkv, full = heads * paged_most_cuts(B, Hkv, most, whole), slots = paged_slots(heads) + (paged_at_once(heads) ? 0 : heads);
     return (int)(full < slots ? full : slots);
 }
 
-bool paged_joins(int B, int Hkv, int G, int64_t most) { return paged_most_cuts(B, Hkv, most) * G <= PAGED_JOIN; }
+bool paged_joins(int B, int Hkv, int G, int64_t most, int whole) { return paged_most_cuts(B, Hkv, most, whole) * G <= PAGED_JOIN; }
 
 hipError_t init_paged_kernels() {
     hipError_t e;

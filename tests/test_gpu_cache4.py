@@ -337,3 +337,18 @@ def test_what_the_binding_refuses():
     rows = torch.zeros(2, 2, 64, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(binding.LoopServeError, match="differ"):          # d of the shape is 64, and of the pages 128
         ctx.ls_cache_write(binding.make_shape(1, 2, 2, 64, 1, 2, 1, "bf16"), cache, rows, rows, _i32([[0]]), starts=_i32([0, 2]))
+
+
+@pytest.mark.parametrize("B,Hkv,Hq,n", [(16, 8, 8, 1632), (16, 8, 8, 1633), (127, 1, 2, 513), (127, 1, 2, 512), (40, 4, 4, 2048), (40, 4, 8, 2049), (70, 2, 2, 1792), (70, 2, 2, 1793)])
+def test_heads_that_stay_whole(B, Hkv, Hq, n):
+    """Sequences at either side of the length from which their heads are cut, which goes by how many heads there are."""
+    rng = np.random.default_rng(B + n)
+    lens = [int(x) for x in rng.integers(0, 40, B)]
+    lens[3], lens[B - 1] = n, n - 1
+    pages = sum(-(-x // 64) for x in lens)
+    p = p4.pool(rng, pages, Hkv, 64, 64)
+    q, table = pu.rnd(rng, B, Hq, 64, scale=1.5), pu.table_for(rng, lens, 64, pages)
+    print("paged4 whole", B, Hkv, Hq, n, flush=True)
+    out, lse, status = _attend(p, q, table, lens, times=3)
+    assert status == 0
+    _check(p, q, table, lens, out, lse)
