@@ -214,7 +214,7 @@ struct RotateArgs {
     int dims, neighbours;
     float eps;
     int B, n_hat, Hq, Hkv;
-    int heads, splits;        // of a row in all, V's among them; groups of lanes that a row's heads are shared out among
+    int heads, each, chunk;   // of a row in all, V's among them; a workgroup's rows, and heads
     int64_t group0;           // first workgroup of this launch
     int32_t* status;
 };

@@ -61,6 +61,10 @@ CASES = [
     (3000, 16, 4, 128, 128, True, "qk", 1e6),
     (5003, 6, 2, 64, 64, False, "qk", 1e4),
     (700, 33, 11, 64, 32, False, "q", 1e4),
+    (3, 256, 2, 128, 128, False, "qk", 1e4),               # more heads than a workgroup takes
+    (201, 500, 4, 64, 64, True, "qk", 1e4),
+    (20000, 1, 1, 64, 64, False, "k", 1e4),                # few of many rows
+    (2500, 40, 8, 128, 64, True, "qk", 1e4),
 ]
 
 
@@ -260,9 +264,9 @@ def test_far_and_negative_positions(neighbours):
         _check(got, _expect(x, None, 0, freq, positions, neighbours), torch.float32)
 
 
-def test_more_rows_than_a_launch_has_threads_for():
-    """Rows of a query and a key head whose items take more than 2^32 threads (queries in, keys and values share one place in memory): the first and the last ones are right."""
-    n, d = 357913941 + 1003, 64
+def test_more_rows_than_a_launch_has_workgroups_for():
+    """Rows of a query and a key head, 64 to a workgroup, that take a second launch (queries in, keys and values share one place in memory): the first and the last ones are right."""
+    n, d = (1 << 29) + 1003, 64
     rng = np.random.default_rng(9)
     freq, w, rotation = _rotation(rng, d, d, False, "qk", 1e4)
     q, k, v = (pu.rnd(rng, 1, 1, d) for _ in range(3))
