@@ -340,7 +340,7 @@ int ls_cache_read(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, con
  * ls_cache_resize -- sequences that grow and shrink: pages for them from a ring of free ones and back to it, and for the rows that a step adds what the other calls
  * take.  Once a step, for all layers whose pools are alike (they share the table).
  *
- *   shape: B sequences, Hkv and d of the cache; n_hat >= 1: rows that positions and slots have room for.  Hq, n, w, dtype, scale are as elsewhere, and ignored.
+ *   shape: B sequences, Hkv and d of the cache; n_hat >= 1: rows that positions and slots have room for, in all or of each sequence.  Hq, n, w, dtype, scale are ignored.
  *   cache: of which `page` and `pages` are used
  *   free_pages [pages] int32, state [2] int32: a ring.  The numbers of the free pages are its `state[1]` entries from entry state[0] on, and behind the last entry comes
  *        the first.  (In the beginning: 0 .. pages - 1, and {0, pages}.)
@@ -352,10 +352,11 @@ int ls_cache_read(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, con
  *   Pages that several sequences share are each sequence's here: give them back once.
  * Outputs (device memory; new_len and new_state may be len and state themselves):
  *   new_len [B], new_state [2], table, free_pages
- *   starts [B+1] int32 or NULL: the rows of the step, packed: sequence b adds rows starts[b] .. starts[b+1] - 1, add[b] of them where that is positive (also where it
+ *   starts [B+1] int32: the rows of the step, packed: sequence b adds rows starts[b] .. starts[b+1] - 1, add[b] of them where that is positive (also where it
  *        does not grow).  A sequence whose rows go beyond n_hat has none and does not grow, like all behind it (LS_STAT_STARTS).
- *   positions [n_hat] int32 or NULL: of each row, 0 where its sequence does not grow and behind the last sequence
- *   slots [n_hat] int64 or NULL: page * (positions of a page) + place in it of each row, as ls_norm_rotate takes it; -1 there
+ *        NULL: each sequence has n_hat rows of its own, of which it adds the first add[b]; one that would add more does not grow (LS_STAT_STARTS).
+ *   positions int32, slots int64 ([n_hat], without starts [B,n_hat]), or NULL: of each row its position, and page * (positions of a page) + place in it, as
+ *        ls_norm_rotate takes them; 0 and -1 of rows whose sequence does not grow, that it does not add, and behind the last sequence
  * No workspace.
  */
 int ls_cache_resize(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, int32_t* free_pages, const int32_t* state, int32_t* new_state,

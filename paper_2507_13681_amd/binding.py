@@ -360,7 +360,7 @@ class Context:
             self._check(rc)
 
     def ls_cache_resize(self, shape, cache, free, state, add, lens, table, new_state=None, new_lens=None, starts=None, positions=None, slots=None):
-        """free, state, lens and table as alloc_pages makes them.  new_state, new_lens None: state and lens are updated."""
+        """free, state, lens and table as alloc_pages makes them.  new_state, new_lens None: state and lens are updated.  positions, slots: [rows] with starts, [B, rows] without."""
         rc = self.pages.cache_resize(self.hv, self.device, shape, self._pages(cache), free, state, state if new_state is None else new_state, add, lens,
                                      lens if new_lens is None else new_lens, table, starts, positions, slots)
         if rc:

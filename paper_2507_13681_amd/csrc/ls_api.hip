@@ -737,7 +737,7 @@ Wrong check_resize(const ls_shape* s, const ls_cache* cache, const int32_t* free
                    const int32_t* len, const int32_t* new_len, const int32_t* table, int32_t max_pages, const int32_t* starts, const int32_t* positions, const int64_t* slots) {
     Wrong w = check_heads(s, false);
     if (w.code) return w;
-    if (s->n_hat < 1 || s->n_hat > MOST_ROWS) return {LS_ESHAPE, "rows out of range"};
+    if (s->n_hat < 1 || s->n_hat > MOST_ROWS || (!starts && s->B * s->n_hat > MOST_ROWS)) return {LS_ESHAPE, "rows out of range"};
     if ((w = check_cache(cache, s, table, max_pages)).code) return w;
     if (!free_pages || !state || !new_state || !add || !len || !new_len) return {LS_EINVAL, "NULL tensor"};
     for (const int32_t* p : {free_pages, state, new_state, add, len, new_len, table, starts, positions})

@@ -146,8 +146,11 @@ PyObject* cache_resize(PyObject*, PyObject* const* a, Py_ssize_t nargs) {       
         int32_t *state = words(5, "state", 2), *new_state = words(6, "new_state", 2), *add = words(7, "add", s.B), *len = words(8, "lens", s.B), *new_len = words(9, "new_lens", s.B);
         int32_t max_pages = 0;
         int32_t* table = static_cast<int32_t*>(plain(a[10], "table", I32, c.device, {s.B, -1}, &max_pages));
-        int32_t *starts = words(11, "starts", (int64_t)s.B + 1), *positions = words(12, "positions", s.n_hat);
-        int64_t* slots = static_cast<int64_t*>(plain(a[13], "slots", at::kLong, c.device, {s.n_hat}));
+        const bool packed = a[11] != Py_None;
+        int32_t* starts = words(11, "starts", (int64_t)s.B + 1);
+        auto rows = [&](int i, const char* name, at::ScalarType type) { return packed ? plain(a[i], name, type, c.device, {s.n_hat}) : plain(a[i], name, type, c.device, {s.B, s.n_hat}); };
+        int32_t* positions = static_cast<int32_t*>(rows(12, "positions", I32));
+        int64_t* slots = static_cast<int64_t*>(rows(13, "slots", at::kLong));
         return released([&] { return ls_cache_resize(c.ctx, &s, &cache, free_pages, state, new_state, add, len, new_len, table, max_pages, starts, positions, slots, c.stream); });
     });
 }

@@ -28,6 +28,7 @@ __device__ __forceinline__ uint32_t row_upto(uint32_t x) {
 
 constexpr int RESIZE_WAVES = 16, RESIZE_THREADS = 64 * RESIZE_WAVES, RESIZE_ALONE = 4 * RESIZE_THREADS;
 
+template <bool PACKED>
 __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a) {
     constexpr int WAVES = RESIZE_WAVES, THREADS = RESIZE_THREADS, MANY = 0x7FFFFFFF;
     enum { GIVE, TAKE, ROWS };
@@ -92,7 +93,7 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
             give_to = join(GIVE, g, give0);
             if (tid == 0) given_s = give0;
         }
-        const bool fits = rows_to <= a.n_rows, wants = ok && add > 0 && fits && now <= most;
+        const bool fits = PACKED ? rows_to <= a.n_rows : add <= a.n_rows, wants = ok && add > 0 && fits && now <= most;
         const int need = wants ? pages_of(now) - pages_of(old) : 0;
         if (live) d = lanes_upto64((uint32_t)need);
         if (lane == 63) waves_s[TAKE][wv] = d;
@@ -105,7 +106,7 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
             if (add > 0 && !fits) odd |= STAT_STARTS;
             if (wants && !grows) odd |= STAT_PAGES_OUT;
             // how far rows and pages go: the sums rise, so that those which are of account are the first ones
-            const uint64_t fit = __ballot(fits), got = __ballot(need > 0 && grows);
+            const uint64_t fit = __ballot(PACKED && fits), got = __ballot(need > 0 && grows);
             if (fit && lane == 63 - __builtin_clzll(fit)) atomicMax(&fits_s, (int)rows_to);
             if (got && lane == 63 - __builtin_clzll(got)) atomicMax(&taken_s, (int)need_to);
             upto_s[TAKE][tid] = need_to <= count ? (int)need_to : MANY;
@@ -114,31 +115,34 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
         } else {
             upto_s[TAKE][tid] = MANY;
         }
-        upto_s[ROWS][tid] = live && fits ? (int)rows_to : MANY;
+        upto_s[ROWS][tid] = !PACKED ? (grows ? add : 0) : live && fits ? (int)rows_to : MANY;            // (padded: how many are its own)
         upto_s[GIVE][tid] = live && give_to < MANY ? (int)give_to : MANY;
         __syncthreads();
         fits0 = fits_s > fits0 ? fits_s : fits0;
         taken0 = taken_s > taken0 ? taken_s : taken0;
         give0 = given_s;
         if (a.finish && first && tid < here) {
-            if (a.starts) a.starts[b + 1] = fits ? (int)rows_to : fits0;
+            if (PACKED) a.starts[b + 1] = fits ? (int)rows_to : fits0;
             a.new_len[b] = grows || shrinks ? (int)now : old;
         }
         if (a.bulk) {
             // ---- the pages and rows of these sequences, one behind the other: whose one is, its number there, and the page number that it is about, which lies in
             // the ring or in the table
             const int64_t gives = (give0 < spare ? give0 : spare) - give1, n_give = gives > 0 ? gives : 0, n_take = taken0 - taken1;
-            const int64_t items = n_give + n_take + (a.positions || a.slots ? fits0 - fits1 : 0);
+            const int64_t items = n_give + n_take + (!a.positions && !a.slots ? 0 : PACKED ? fits0 - fits1 : here * a.n_rows);
             int top = 1;
             while (top < here) top *= 2;
             for (int64_t y = (int64_t)turn * THREADS + tid; y < items; y += step) {
-                const int kind = y < n_give ? GIVE : y < n_give + n_take ? TAKE : ROWS, before = kind == GIVE ? (int)give1 : kind == TAKE ? taken1 : fits1;
+                const int kind = y < n_give ? GIVE : y < n_give + n_take ? TAKE : ROWS, before = kind == GIVE ? (int)give1 : kind == TAKE ? taken1 : PACKED ? fits1 : 0;
                 const int x = (int)(before + y - (kind == GIVE ? 0 : kind == TAKE ? n_give : n_give + n_take));
                 const int* upto = upto_s[kind];
                 int t = 0;
-                for (int s = top / 2; s > 0; s /= 2) t += upto[t + s - 1] <= x ? s : 0;           // (entries behind the last sequence are all there is, which is more than x)
-                const int i = x - (t ? upto[t - 1] : before), had = old_s[t], from = from_s[t];
+                if (!PACKED && kind == ROWS) t = x / a.n_rows;
+                else for (int s = top / 2; s > 0; s /= 2) t += upto[t + s - 1] <= x ? s : 0;           // (entries behind the last sequence are all there is, which is more than x)
+                const int i = x - (!PACKED && kind == ROWS ? t * a.n_rows : t ? upto[t - 1] : before), from = from_s[t];
                 if (kind == ROWS) {
+                    const int64_t at = PACKED ? x : (int64_t)b0 * a.n_rows + x;
+                    const int had = PACKED || i < upto[t] ? old_s[t] : -1;
                     int64_t slot = -1;
                     const int p = had < 0 ? 0 : had + i, nth = p >> a.page_log;
                     if (had >= 0 && a.slots) {
@@ -146,8 +150,8 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
                         if ((uint32_t)page < (uint32_t)a.pages) slot = ((int64_t)page << a.page_log) + (p & ((1 << a.page_log) - 1));
                         else bad = STAT_PAGE_RANGE;
                     }
-                    if (a.positions) a.positions[x] = p;
-                    if (a.slots) a.slots[x] = slot;
+                    if (a.positions) a.positions[at] = p;
+                    if (a.slots) a.slots[at] = slot;
                 } else {
                     int32_t* const entry = a.table + (int64_t)(b0 + t) * a.max_pages + from + i;
                     int32_t* const place = a.free + (kind == GIVE ? ring(tail, x) : ring(head, x));
@@ -159,7 +163,7 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
         turn = turn ? turn - 1 : gridDim.x - 1;
         if (b0 + THREADS < a.B) __syncthreads();
     }
-    if (a.bulk)                                                // rows of no sequence
+    if (a.bulk && PACKED)                                      // rows of no sequence
         for (int64_t x = fits0 + me; x < a.n_rows; x += step) {
             if (a.positions) a.positions[x] = 0;
             if (a.slots) a.slots[x] = -1;
@@ -167,7 +171,7 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
     if (give0 > spare) odd |= STAT_PAGE_RANGE;
     if (a.finish && first) {
         if (tid == 0) {
-            if (a.starts) a.starts[0] = 0;
+            if (PACKED) a.starts[0] = 0;
             const int given = give0 < spare ? (int)give0 : spare;
             a.new_state[0] = ring(head, taken0);
             a.new_state[1] = count - taken0 + given;
@@ -179,15 +183,19 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
 
 hipError_t run_resize(ResizeArgs a, hipStream_t st) {
     const bool in_place = a.new_len == a.len || a.new_state == a.state;
-    const int64_t groups = (a.n_rows + RESIZE_THREADS - 1) / RESIZE_THREADS;
+    const int64_t rows = a.starts ? a.n_rows : (int64_t)a.B * a.n_rows, groups = (rows + RESIZE_THREADS - 1) / RESIZE_THREADS;
     // In place one workgroup does it alone up to here: a launch more takes 4 us.
-    const int grid = in_place && a.n_rows <= RESIZE_ALONE ? 1 : groups < 256 ? (int)groups : 256;
+    const int grid = in_place && rows <= RESIZE_ALONE ? 1 : groups < 256 ? (int)groups : 256;
     a.bulk = 1;
     a.finish = grid == 1 || !in_place;
-    hipLaunchKernelGGL(resize_kernel, dim3(grid), dim3(RESIZE_THREADS), 0, st, a);
+    auto launch = [&](int n) {
+        if (a.starts) hipLaunchKernelGGL((resize_kernel<true>), dim3(n), dim3(RESIZE_THREADS), 0, st, a);
+        else hipLaunchKernelGGL((resize_kernel<false>), dim3(n), dim3(RESIZE_THREADS), 0, st, a);
+    };
+    launch(grid);
     if (!a.finish) {
         a.bulk = 0; a.finish = 1;
-        hipLaunchKernelGGL(resize_kernel, dim3(1), dim3(RESIZE_THREADS), 0, st, a);
+        launch(1);
     }
     return hipGetLastError();
 }

@@ -10,8 +10,8 @@ pytestmark = pytest.mark.gpu
 OUT, RANGE, STARTS = binding.LS_STAT_PAGES_OUT, binding.LS_STAT_PAGE_RANGE, binding.LS_STAT_STARTS
 
 
-def expect(free, state, add, lens, table, page, n_rows):
-    """(dict of all outputs, status) from numpy arrays."""
+def expect(free, state, add, lens, table, page, n_rows, padded=False):
+    """(dict of all outputs, status) from numpy arrays; padded: n_rows of each sequence."""
     free, table, new = free.copy(), table.copy(), lens.astype(np.int64).copy()
     pages, room = len(free), min(table.shape[1] * page, 2 ** 31 - 1)
     head, count, status = int(state[0]), int(state[1]), 0
@@ -19,7 +19,8 @@ def expect(free, state, add, lens, table, page, n_rows):
         head = count = 0
         status |= RANGE
     was = free.copy()
-    starts, positions, slots = [0], np.zeros(n_rows, np.int32), np.full(n_rows, -1, np.int64)
+    room_for = len(lens) * n_rows if padded else n_rows
+    starts, positions, slots = [0], np.zeros(room_for, np.int32), np.full(room_for, -1, np.int64)
     asked = taken = given = 0
     full = False
     for b in range(len(lens)):
@@ -27,14 +28,14 @@ def expect(free, state, add, lens, table, page, n_rows):
         now, ok = max(0, old + by), 0 <= old <= room
         have, want = -(-old // page), -(-now // page)
         rows = max(by, 0)
-        full = full or sum_rows(starts, rows) > n_rows
+        full = rows > n_rows if padded else full or starts[-1] + rows > n_rows
         if not ok:
             status |= RANGE
         if rows and full:
             status |= STARTS
             rows = 0
-        first = starts[-1]
-        starts.append(first + rows)
+        first = b * n_rows if padded else starts[-1]
+        starts.append(starts[-1] + rows)
         if ok and by < 0:
             for j in range(want, have):
                 if given < pages - count:
@@ -64,11 +65,8 @@ def expect(free, state, add, lens, table, page, n_rows):
             slots[first:first + rows] = np.where(good, at * page + p % page, -1)
     given = min(given, pages - count)
     state = np.array([(head + taken) % pages, count - taken + given], np.int32)
-    return dict(free=free, state=state, lens=new.astype(np.int32), table=table, starts=np.array(starts, np.int32), positions=positions, slots=slots), status
-
-
-def sum_rows(starts, rows):
-    return starts[-1] + rows
+    shape = (len(lens), n_rows) if padded else (n_rows,)
+    return dict(free=free, state=state, lens=new.astype(np.int32), table=table, starts=np.array(starts, np.int32), positions=positions.reshape(shape), slots=slots.reshape(shape)), status
 
 
 class Server:
@@ -86,13 +84,16 @@ class Server:
             self.host[n] = np.array(x, np.int32).reshape(self.host[n].shape)
             self.dev[n].copy_(torch.from_numpy(self.host[n]))
 
-    def step(self, add, n_rows=None, without=()):
-        B = len(add)
-        n_rows = n_rows or max(1, int(np.maximum(add, 0).astype(np.int64).sum()))
+    def step(self, add, n_rows=None, without=(), padded=False):
+        """without starts: padded"""
+        B, padded = len(add), padded or "starts" in without
+        without = tuple(without) + (("starts",) if padded else ())
+        n_rows = n_rows or max(1, int(np.maximum(add, 0).max() if padded else np.maximum(add, 0).astype(np.int64).sum()))
         d, h = self.dev, self.host
-        want, status = expect(h["free"], h["state"], np.array(add), h["lens"], h["table"], self.page, n_rows)
+        want, status = expect(h["free"], h["state"], np.array(add), h["lens"], h["table"], self.page, n_rows, padded)
         shape = binding.make_shape(B, 1, 1, 64, 1, n_rows, 1, "bf16")
-        rows = dict(starts=_i32([77] * (B + 1)), positions=_i32([77] * n_rows), slots=torch.full((n_rows,), 77, dtype=torch.int64, device="cuda"))
+        size = (B, n_rows) if padded else (n_rows,)
+        rows = dict(starts=_i32([77] * (B + 1)), positions=torch.full(size, 77, dtype=torch.int32, device="cuda"), slots=torch.full(size, 77, dtype=torch.int64, device="cuda"))
         new = {} if self.in_place else dict(new_state=_i32([77, 77]), new_lens=_i32([77] * B))
         self.ctx.ls_cache_resize(shape, self.cache, d["free"], d["state"], _i32([int(x) for x in add]), d["lens"], d["table"], **new,
                                  **{n: None if n in without else x for n, x in rows.items()})
@@ -122,7 +123,11 @@ def test_a_server(B, page, pages, max_pages, in_place):
         kind = rng.choice(5, B, p=[0.15, 0.5, 0.15, 0.1, 0.1])
         new = rng.integers(1, max(2, 2 * pages * page // B), B)
         add = np.where(kind == 0, new, np.where(kind == 1, 1, np.where(kind == 2, -lens, np.where(kind == 3, -rng.integers(1, 3 * page, B), 0))))
-        _, status = s.step(add, n_rows=max(1, int(np.maximum(add, 0).sum()) + int(rng.choice([0, 1, 100, -3]))), without=("positions",) if i == 5 else ("slots",) if i == 6 else ("starts",) if i == 7 else ())
+        if i % 4 == 3:                                         # each sequence has rows of its own
+            _, status = s.step(add, n_rows=max(1, int(np.maximum(add, 0).max()) + int(rng.choice([0, 1, 7, -3]))), without=("positions",) if i == 7 else ("slots",) if i == 11 else (), padded=True)
+            seen |= status
+            continue
+        _, status = s.step(add, n_rows=max(1, int(np.maximum(add, 0).sum()) + int(rng.choice([0, 1, 100, -3]))), without=("positions",) if i == 5 else ("slots",) if i == 6 else ())
         seen |= status
     held = s.host["table"][np.arange(max_pages)[None] < -(-s.host["lens"] // page)[:, None]]
     head, count = s.host["state"]
@@ -197,6 +202,10 @@ def test_sums_beyond_32_bits(in_place):
     add[7] = 300
     _, status = s.step(add, n_rows=9001)
     assert status == 0 and s.host["lens"][0] == 0 and s.host["lens"][7] == 300
+    add = np.full(B, 2147483647, np.int64)
+    add[11], add[13] = 40, 400
+    _, status = s.step(add, n_rows=400, padded=True)
+    assert status == STARTS and s.host["lens"][11] == 40 and s.host["lens"][13] == 400
 
 
 def test_as_many_sequences_as_there_can_be():
@@ -207,6 +216,7 @@ def test_as_many_sequences_as_there_can_be():
     print("resize 65535", flush=True)
     s.step(add)
     s.step(np.where(rng.random(B) < 0.5, -s.host["lens"], 16 - s.host["lens"]))
+    s.step(np.where(s.host["lens"] == 16, rng.integers(-16, 1, B), rng.integers(-2, 17, B)), padded=True)
 
 
 def test_a_captured_decode_loop():
@@ -243,8 +253,9 @@ def test_what_the_binding_refuses():
     add, i64 = _i32([1, 0, 0]), torch.zeros(5, dtype=torch.int64, device="cuda")
     call = lambda free=d["free"], state=d["state"], add=add, lens=d["lens"], table=d["table"], **kw: s.ctx.ls_cache_resize(shape, s.cache, free, state, add, lens, table, **kw)
     call(slots=i64, positions=_i32([0] * 5), starts=_i32([0] * 4))
+    call(slots=i64[None].expand(3, 5).contiguous(), positions=_i32([[0] * 5] * 3))
     for kw in (dict(free=d["free"][:7]), dict(state=_i32([0, 8, 0])), dict(add=add.long()), dict(add=add.cpu()), dict(lens=_i32([0] * 4)), dict(table=d["table"][:2]), dict(table=d["table"].t()),
-               dict(slots=i64.int()), dict(slots=i64[:4]), dict(positions=i64), dict(starts=_i32([0] * 3)), dict(new_lens=_i32([0] * 2))):
+               dict(slots=i64.int()), dict(slots=i64[:4]), dict(slots=i64), dict(positions=i64), dict(starts=_i32([0] * 4), slots=i64[None].expand(3, 5).contiguous()), dict(starts=_i32([0] * 3)), dict(new_lens=_i32([0] * 2))):
         with pytest.raises(ValueError):
             call(**kw)
     both = _i32([0] * 4)

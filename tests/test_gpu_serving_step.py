@@ -69,9 +69,11 @@ class Server:
                 pu.check(out[b, g].cpu(), lse[b, g].cpu(), ref, torch.bfloat16)
 
 
+@pytest.mark.parametrize("padded", [False, True])
 @pytest.mark.parametrize("kind", ["bf16", "e4m3", "e2m1"])
-def test_steps_of_a_server(kind):
-    print("serving step", kind, flush=True)
+def test_steps_of_a_server(kind, padded):
+    """padded: in the decode steps each dialogue has a row of its own, whether it goes on or not."""
+    print("serving step", kind, padded, flush=True)
     B = 4
     s = Server(B, kind, 21)
     # ---- two prompts, in a step padded to a fixed number of rows
@@ -95,14 +97,19 @@ def test_steps_of_a_server(kind):
             pu.check(out[rows, h].cpu(), lse[h, rows].cpu(), ref, torch.bfloat16)
     # ---- a decode step, recorded: a row for each dialogue that goes on, none for the others
     by, at = _i32([0] * B), dict(starts=_i32([0] * (B + 1)), positions=_i32([0] * B), slots=torch.zeros(B, dtype=torch.int64, device="cuda"))
+    if padded:
+        at = dict(starts=None, positions=at["positions"][:, None], slots=at["slots"][:, None])
+    rows_of = _i32([0, 1, 2, 3]) if padded else at["starts"]
+    seen = (lambda x: x[:, :, None]) if padded else (lambda x: x)
     qkv = torch.zeros(B, HQ + 2 * HKV, D, dtype=torch.bfloat16, device="cuda")
     rq, rk = torch.zeros(B, HQ, D, dtype=torch.bfloat16, device="cuda"), torch.zeros(B, HKV, D, dtype=torch.bfloat16, device="cuda")
     out, lse = torch.zeros_like(rq), torch.zeros(B, HQ, device="cuda")
-    one = binding.make_shape(B, HQ, HKV, D, MOST * PAGE, B, 1, "bf16")
+    one = binding.make_shape(B, HQ, HKV, D, MOST * PAGE, 1 if padded else B, 1, "bf16")
 
     def step():
         s.ctx.ls_cache_resize(one, s.cache, s.at["free"], s.at["state"], by, s.at["lens"], s.at["table"], **at)
-        s.ctx.ls_norm_rotate(one, s.rotation, qkv[:, :HQ], qkv[:, HQ:HQ + HKV], rq, rk, at["positions"], s.cache, qkv[:, HQ + HKV:], at["slots"])
+        q, k, v = seen(qkv[:, :HQ]), seen(qkv[:, HQ:HQ + HKV]), seen(qkv[:, HQ + HKV:])
+        s.ctx.ls_norm_rotate(one, s.rotation, q, k, seen(rq), seen(rk), at["positions"], s.cache, v, at["slots"])
         s.ctx.ls_paged_attend(one, s.cache, rq, s.at["table"], s.at["lens"], out, lse)
 
     step()                                                 # (nobody grows)
@@ -111,13 +118,13 @@ def test_steps_of_a_server(kind):
     with torch.cuda.graph(graph):
         step()
     for i in range(24):
-        add = [1, 1, 1, int(i >= 10)]
+        add = [1, int(not padded or i % 3 != 1), 1, int(i >= 10)]
         by.copy_(torch.tensor(add, dtype=torch.int32))
         qkv.copy_(pu.rnd(s.rng, *qkv.shape))
         torch.cuda.synchronize()
         graph.replay()
         assert s.ctx.ls_poll_status() == 0
-        s.keep(add, rk, qkv[:, HQ + HKV:], at["starts"])
+        s.keep(add, rk, qkv[:, HQ + HKV:], rows_of)
         if i in (0, 9, 10, 23):                            # (before the fourth has a row the queries' rows are the dialogues')
             s.check_tokens(rq, out, lse)
     # ---- one is cut, one ends, and another prompt finds room in what they gave back
@@ -128,15 +135,15 @@ def test_steps_of_a_server(kind):
     s.ctx.ls_norm_rotate(binding.make_shape(B, HQ, HKV, D, 1, 64, 1, "bf16"), s.rotation, q, k, rq2, rk2, at2["positions"], s.cache, v, at2["slots"])
     assert s.ctx.ls_poll_status() == 0
     s.keep(add, rk2, v, at2["starts"])
-    assert [len(x) for x in s.k] == [54, 84, 0, 14]
+    assert [len(x) for x in s.k] == [54, 76 if padded else 84, 0, 14]
     for i in range(3):
         by.copy_(torch.tensor([1, 1, 0, 1], dtype=torch.int32))
         qkv.copy_(pu.rnd(s.rng, *qkv.shape))
         torch.cuda.synchronize()
         graph.replay()
         assert s.ctx.ls_poll_status() == 0
-        s.keep([1, 1, 0, 1], rk, qkv[:, HQ + HKV:], at["starts"])
-    s.check_tokens(rq, out, lse)
+        s.keep([1, 1, 0, 1], rk, qkv[:, HQ + HKV:], rows_of)
+    s.check_tokens(rq, out, lse)                           # (packed rows of a step in which one is idle are not the dialogues': a query is a query)
     # ---- a context back in order, as the scoring and the retention take it
     n = len(s.k[1])
     back = [torch.zeros(1, HKV, n, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]

@@ -14,6 +14,7 @@ RESIZE = [
     (dict(max_pages=0), ESHAPE), (dict(max_pages=-3), ESHAPE), (dict(cache=dict(page=12)), ESHAPE), (dict(cache=dict(pages=2 ** 31)), ESHAPE), (dict(cache=dict(pages=2 ** 31 - 1)), 0),
     (dict(cache=dict(type=4)), 0), (dict(cache=dict(type=7)), EINVAL), (dict(cache=dict(Hkv=3)), ESHAPE),
     (dict(shape=dict(n_hat=0)), ESHAPE), (dict(shape=dict(n_hat=2 ** 31)), ESHAPE), (dict(shape=dict(B=0)), ESHAPE), (dict(shape=dict(B=17000)), ESHAPE), (dict(shape=dict(Hq=0)), 0),
+    (dict(shape=dict(n_hat=2147483000)), 0), (dict(starts=None, shape=dict(n_hat=2147483000)), ESHAPE), (dict(starts=None, shape=dict(n_hat=1073741500)), 0),
 ]
 
 
