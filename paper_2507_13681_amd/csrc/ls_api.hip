@@ -808,9 +808,10 @@ Wrong check_packed(const ls_shape* s, const ls_rows* q, const ls_rows* k, const 
 ls::PackedCut packed_cut(const ls_shape* s, bool packed, size_t room) {
     return ls::packed_cut(s->B, packed, s->n, s->n_hat, s->Hkv, s->Hq / s->Hkv, s->dtype, s->d, (int64_t)(room / ls::prefill_slot_bytes(s->d)));
 }
-size_t paged_bytes(const ls_shape* s) {
+size_t paged_part_bytes(const ls_shape* s) { return up((size_t)ls::paged_units(s->B, s->Hkv, s->n) * (s->Hq / s->Hkv) * ls::decode_part_floats(s->d) * 4); }
+size_t paged_bytes(const ls_shape* s) {                    // parts' results, and where each head's are
     if (ls::paged_most_cuts(s->B, s->Hkv, s->n) == 1) return 0;
-    return up((size_t)ls::paged_units(s->B, s->Hkv, s->n) * (s->Hq / s->Hkv) * ls::decode_part_floats(s->d) * 4);
+    return paged_part_bytes(s) + up((size_t)s->B * s->Hkv * sizeof(int2));
 }
 }  // namespace
 
@@ -895,14 +896,15 @@ int ls_paged_attend(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const v
     a.cache = cache_args(cache, table, max_pages);
     a.q = q; a.len = len; a.out = out; a.lse = lse; a.part = reinterpret_cast<float*>(c->ws);
     a.B = s->B; a.Hq = s->Hq; a.Hkv = s->Hkv; a.G = s->Hq / s->Hkv; a.most = s->n; a.scale_log2e = scale_log2e(s); a.status = c->status;
-    a.whole = ls::paged_whole(cache->type, (int64_t)s->B * s->Hkv);
-    const bool joins = ls::paged_joins(s->B, s->Hkv, a.G, s->n, a.whole), counts = joins && ls::paged_most_cuts(s->B, s->Hkv, s->n, a.whole) > 1;
+    a.four = cache->type == LS_CACHE_E2M1;
+    a.heads = reinterpret_cast<int2*>(c->ws + paged_part_bytes(s));
+    const bool joins = ls::paged_joins(s->B, s->Hkv, a.G, s->n, a.four), counts = joins && ls::paged_most_cuts(s->B, s->Hkv, s->n, a.four) > 1;
     a.done = joins ? decode_set(c, c->decode_calls) : nullptr;
     a.done_clear = decode_set(c, c->decode_calls + 2);
     a.clear_heads = !counts ? 0 : c->decode_heads > s->B * s->Hkv ? c->decode_heads : s->B * s->Hkv;
     const OnDevice on(c->device);
     if (!on.ok) return fail(c, LS_EHIP, "ls_paged_attend: hipSetDevice failed");
-    const hipError_t e = ls::run_paged(a, cache->type, s->d, ls::paged_units(s->B, s->Hkv, s->n, a.whole), static_cast<hipStream_t>(stream));
+    const hipError_t e = ls::run_paged(a, cache->type, s->d, ls::paged_units(s->B, s->Hkv, s->n, a.four), static_cast<hipStream_t>(stream));
     if (counts) { ++c->decode_calls; c->decode_heads = a.clear_heads; }
     if (e != hipSuccess) return fail(c, LS_EHIP, "ls_paged_attend: %s", hipGetErrorString(e));
     return LS_OK;

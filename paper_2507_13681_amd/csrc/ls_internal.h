@@ -240,24 +240,28 @@ __host__ __device__ inline bool paged_at_once(int64_t heads) { return heads * 4 
 // Tiles that a head is not cut for, two a wave.  Whole / in parts, us: 32 tiles 14.3 / 8.9, 17 tiles 9.8 / 8.7, 10 tiles 7.1 / 8.3, 16 tiles of 32 sequences 10.6 / 14.0
 constexpr int PAGED_WHOLE = 16;
 constexpr int PAGED_SHORTEST = 4, PAGED_SHORTEST_MANY = 32;                          // tiles of a part at least; of that many heads
-// .. of e2m1 pages, whose tiles are read sooner, and more of many heads, which fill the chip whole.  Whole / in parts, us, sequences of 8 KV heads: 16 of 1000 11.0 / 12.5, of 2040 16.8 / 15.3, 20 of 1800
-// 15.6 / 16.1, 32 of them 16.0 / 19.4, 48 of 2040 26.3 / 27.1; 4 of 1500 13.6 / 9.9
-constexpr int PAGED_MANY_4 = 128, PAGED_WHOLE_4 = 64;
-__host__ __device__ inline int paged_whole(int type, int64_t heads) {
-    if (type != CACHE_E2M1 || heads < PAGED_MANY_4) return PAGED_WHOLE;
-    return heads * 2 / 5 < PAGED_WHOLE_4 ? (int)(heads * 2 / 5) : PAGED_WHOLE_4;
-}
 __host__ __device__ inline int paged_cuts(int tiles, int length, int whole = PAGED_WHOLE) { return tiles <= whole ? 1 : (int)(((uint32_t)tiles + (uint32_t)length - 1) / (uint32_t)length); }
+// .. of e2m1 pages a tile a wave: a part writes 4 (d + 4) bytes of each query head, which two of these tiles read.  (8 / 4, us: one sequence of 131072, 8 KV heads 35.0 / 36.2; 64 of 0 to 1500, 2 KV heads of 32
+// query heads each 18.4 / 26.1; three drawn batches 9.2 / 10.6, 11.9 / 13.2, 12.2 / 16.0.)
+__host__ __device__ inline int paged_shortest(bool four) { return four ? 8 : PAGED_SHORTEST; }
+// .. and of more than PAGED_ALONE heads stay whole by how long parts are: e2m1 tiles of many heads are sooner done than parts are put together, and what is put together goes by the query heads.  More than 64 tiles
+// are the last to end.  (Whole / cut from 17 tiles on, us, sequences of 8 KV heads: 16 of 1000 10.6 / 12.5, 32 of 1800 15.3 / 18.8; 64 of 0 to 3632 of 4 KV heads 22.9 / 32.0.  64 of 0 to 1500, 2 KV heads of 128 of
+// 32 query heads each: with 8 tiles more / without 18.3 / 28.3.  100 of 0 to 6000, 2 KV heads, up to 64 tiles / up to 79 25.8 / 30.2.)
+__host__ __device__ inline int paged_whole(int64_t heads, int length, int G, bool four) {
+    if (!four || heads <= PAGED_ALONE) return PAGED_WHOLE;
+    const int whole = (G > 16 ? 32 : 24) + length + length / 2;
+    return whole < 64 ? whole : 64;
+}
 // Tiles of a part of a call, of so many tiles in all: what `length` makes of them is counted until it is accepted, four times at most, and then `enough` is taken.  (24 ragged caches of 3212 tiles: 51, 57, 60
 // and 63 tiles are too many parts, 65 would do, 81 are taken.)
 struct PagedLength {
     int length, enough, slots, tries;        // enough: it will do, whatever the sequences are
     bool sorts;                              // not all parts run at once: the longest first
-    __host__ __device__ PagedLength(int64_t tiles, int64_t heads) : slots(paged_slots(heads)), tries(0) {
+    __host__ __device__ PagedLength(int64_t tiles, int64_t heads, bool four = false) : slots(paged_slots(heads)), tries(0) {
         const bool at_once = paged_at_once(heads);
         sorts = !at_once;
         auto least = [&](int64_t parts) {
-            const int64_t each = (tiles + parts - 1) / parts, from = at_once ? PAGED_SHORTEST : PAGED_SHORTEST_MANY;
+            const int64_t each = (tiles + parts - 1) / parts, from = at_once ? paged_shortest(four) : PAGED_SHORTEST_MANY;
             return each < from ? (int)from : each < 1 << 30 ? (int)each : 1 << 30;
         };
         length = least(slots);
@@ -280,11 +284,12 @@ struct PagedArgs {
     float* part;              // [units][G][d + 4] output, reference, normaliser of each part of a head
     uint32_t* done;           // [B*Hkv] parts finished; zero between calls.  Null: paged_join_kernel puts the parts together
     uint32_t* done_clear;     // [clear_heads] the counters of the call after the next, cleared here
+    int2* heads;              // [B*Hkv] first part and parts, for paged4_join_kernel
     int clear_heads;
     int B, Hq, Hkv, G;
     int64_t most;             // no sequence is longer
     float scale_log2e;
-    int whole;                // tiles that a head is not cut for
+    bool four;                // pages are e2m1
     int32_t* status;
 };
 
@@ -389,9 +394,9 @@ hipError_t run_paged(const PagedArgs& a, int type, int d, int units, hipStream_t
 hipError_t init_paged4_kernels();
 hipError_t run_paged4(const PagedArgs& a, int d, int units, hipStream_t st);                 // run_paged of e2m1 pages
 void launch_paged_join(const PagedArgs& a, int d, hipStream_t st);
-int paged_units(int B, int Hkv, int64_t most, int whole = PAGED_WHOLE);                       // workgroups that sequences of up to so many keys take
-bool paged_joins(int B, int Hkv, int G, int64_t most, int whole);                      // the kernel puts parts together itself
-int paged_most_cuts(int B, int Hkv, int64_t most, int whole = PAGED_WHOLE);                   // ... and parts of a head
+int paged_units(int B, int Hkv, int64_t most, bool four = false);                       // workgroups that sequences of up to so many keys take
+bool paged_joins(int B, int Hkv, int G, int64_t most, bool four);                      // the kernel puts parts together itself
+int paged_most_cuts(int B, int Hkv, int64_t most, bool four = false);                   // ... and parts of a head
 hipError_t run_score(const ScoreArgs& a, int dtype, int d, int mode, hipStream_t st);
 hipError_t run_decode(const DecodeArgs& a, int d, hipStream_t st);
 size_t decode_smem_bytes(int d, int G, int nsplit);

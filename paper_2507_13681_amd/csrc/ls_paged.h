@@ -40,6 +40,23 @@ __device__ __forceinline__ bf16x8 bf16_of(uint32_t lo, uint32_t hi, float f) {  
                                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, f, true)}};
     return __builtin_bit_cast(bf16x8, u);
 }
+// Largest over the four rows of 16 lanes, in each of them (through registers; two shuffles through LDS wait a hundred cycles each)
+__device__ __forceinline__ float largest_of_rows(float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto h = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    x = fmaxf(__builtin_bit_cast(float, (uint32_t)h[0]), __builtin_bit_cast(float, (uint32_t)h[1]));
+    const uint32_t v = __builtin_bit_cast(uint32_t, x);
+    const auto q = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return fmaxf(__builtin_bit_cast(float, (uint32_t)q[0]), __builtin_bit_cast(float, (uint32_t)q[1]));
+}
+// n bytes (1, 8 or 16) at a lane's offset from an address that the wave shares: the one in scalar registers, no 64-bit sums of vectors
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+template <typename V>
+__device__ __forceinline__ V load_from(const void* base, uint32_t off) {
+    typedef const __attribute__((address_space(1))) unsigned char* global_t;
+    return *reinterpret_cast<const __attribute__((address_space(1))) V*>((global_t)uniform_ptr(base) + off);
+}
 // eight e2m1 codes times the power of two f
 __device__ __forceinline__ bf16x8 bf16_of4(uint32_t w, float f) {
     struct U { bf16x2 v[4]; } u = {{__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, f, 1),
@@ -65,14 +82,14 @@ struct PagedUnits {
     }
     // f(lane of the sequence in order, parts, units up to and with it, lane of it): called for 64 sequences after the other until it returns true
     template <typename F>
-    __device__ bool walk(const PagedArgs& a, int lane, int whole, F f) {
+    __device__ bool walk(const PagedArgs& a, int lane, bool four, F f) {
         const int64_t room = (int64_t)a.cache.max_pages << a.cache.page_log;
         most = a.most < room ? a.most : room;
         int x = length_of(a, lane);
         int64_t tiles = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64)                   // (64 sequences of 2^31 keys have less than 2^32 tiles)
             tiles += (uint32_t)__builtin_amdgcn_readlane((int)lanes_upto((uint32_t)paged_tiles(b0 ? length_of(a, b0 + lane) : x)), 63);
-        PagedLength l(tiles * a.Hkv, (int64_t)a.B * a.Hkv);
+        PagedLength l(tiles * a.Hkv, (int64_t)a.B * a.Hkv, four);
         if (a.B > 64) l.length = l.enough;
         int before = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64) {
@@ -80,6 +97,7 @@ struct PagedUnits {
             const int here = a.B - b0 < 64 ? a.B - b0 : 64, t = paged_tiles(x);
             int c, upto;
             do {
+                const int whole = paged_whole((int64_t)a.B * a.Hkv, l.length, a.G, four);
                 c = lane < here ? 1 : 0;
                 if (__ballot(t > whole) != 0ull && lane < here) c = paged_cuts(t, l.length, whole);
                 upto = before + (int)lanes_upto((uint32_t)(c * a.Hkv));
@@ -101,9 +119,9 @@ struct PagedUnits {
         }
         return false;
     }
-    __device__ bool find(const PagedArgs& a, int unit, int lane, int whole) {
+    __device__ bool find(const PagedArgs& a, int unit, int lane, bool four) {
         auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-        return walk(a, lane, whole, [&](int b0, int x, int c, int l, int upto) {
+        return walk(a, lane, four, [&](int b0, int x, int c, int l, int upto) {
             const uint64_t in = __ballot(unit < upto);
             if (in == 0ull) return false;
             const int at = __builtin_ctzll(in);
@@ -118,8 +136,8 @@ struct PagedUnits {
             return true;
         });
     }
-    __device__ bool find_head(const PagedArgs& a, int seq, int head, int lane, int whole) {       // the parts of one KV head
-        return walk(a, lane, whole, [&](int b0, int x, int c, int l, int upto) {
+    __device__ bool find_head(const PagedArgs& a, int seq, int head, int lane) {       // the parts of one KV head
+        return walk(a, lane, false, [&](int b0, int x, int c, int l, int upto) {
             const uint64_t in = __ballot(b0 + l == seq);
             if (in == 0ull || seq < b0 || seq >= b0 + 64) return false;
             const int at = __builtin_ctzll(in);
@@ -132,7 +150,7 @@ struct PagedUnits {
 };
 
 template <int D, int NH, int TYPE>
-__global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(PagedArgs a) {
+__global__ __launch_bounds__(PG_THREADS, NH == 1 || (D == 64 && TYPE == CACHE_E2M1) ? 4 : 2) void paged_kernel(PagedArgs a) {
     using C = PagedCfg<D, TYPE>;
     constexpr bool E4M3 = C::E4M3, E2M1 = C::E2M1;
     using T = bf16_t;
@@ -146,9 +164,23 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
 
     // ---- which part of which head this workgroup has
     PagedUnits w;
-    if (!w.find(a, (int)blockIdx.x, lane, E2M1 ? a.whole : PAGED_WHOLE)) return;             // (all waves of the workgroup alike)
+    if constexpr (E2M1) {                                      // one wave for all: the others would take its turns
+        __shared__ PagedUnits unit_s;
+        __shared__ int found_s;
+        if (wv == 0) {
+            const bool found = w.find(a, (int)blockIdx.x, lane, true);
+            if (lane == 0) { unit_s = w; found_s = found; }
+        }
+        __syncthreads();
+        if (!__builtin_amdgcn_readfirstlane(found_s)) return;
+        auto u = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+        w.b = u(unit_s.b); w.kvh = u(unit_s.kvh); w.cut = u(unit_s.cut); w.cuts = u(unit_s.cuts); w.n = u(unit_s.n); w.base = u(unit_s.base); w.most = unit_s.most;
+    } else {
+        if (!w.find(a, (int)blockIdx.x, lane, false)) return;  // (all waves of the workgroup alike)
+    }
     const int b = w.b, kvh = w.kvh, cut = w.cut, cuts = w.cuts, n = w.n;
     const int bk = b * a.Hkv + kvh;
+    if (E2M1 && !a.done && cut == 0 && tid == 0) a.heads[bk] = make_int2(w.base, cuts);
     if (cut == 0 && kvh == 0 && tid == 0 && a.len[b] > w.most) atomicOr(a.status, STAT_PAGE_RANGE);
     const int all = paged_tiles(n), each = (all + cuts - 1) / cuts;
     const int tile0 = cut * each, tend = tile0 + each < all ? tile0 + each : all;
@@ -171,15 +203,20 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
         return Half{((int64_t)(p < 0 ? 0 : p) * a.cache.Hkv << page_log) + head + ((PAGED_TILE * t + 16 * h) & in_page), p >= 0};
     };
     const int trow = lane / C::DS, sl = lane % C::DS;          // a transfer: this lane fills slot sl of tile row RPI * i + trow
-    uint4 vr[2];                                               // e2m1: 32 values of a row of each half (of 64 values, one of both), and their exponent
+    u32x4 vr[2];                                               // e2m1: 32 values of a row of each half (of 64 values, one of both), and their exponent
     uint32_t vrx[2];
     auto request_v = [&](const Half (&hf)[2]) {
         if constexpr (E2M1) {
 #pragma unroll
             for (int i = 0; i < C::NIV; ++i) {
-                const int64_t row = (D == 128 ? hf[i].row : lane < 32 ? hf[0].row : hf[1].row) + (trow & 15);
-                vr[i] = *reinterpret_cast<const uint4*>(a.cache.v + row * C::RB + 16 * sl);
-                vrx[i] = a.cache.vx[row * C::DS + sl];
+                if constexpr (D == 128) {                      // a lane's bytes of 16 rows are neighbours
+                    vr[i] = load_from<u32x4>(a.cache.v + hf[i].row * C::RB, 16u * lane);
+                    vrx[i] = load_from<uint8_t>(a.cache.vx + hf[i].row * C::DS, (uint32_t)lane);
+                } else {
+                    const int64_t row = (lane < 32 ? hf[0].row : hf[1].row) + (trow & 15);
+                    vr[i] = *reinterpret_cast<const u32x4*>(a.cache.v + row * C::RB + 16 * sl);
+                    vrx[i] = a.cache.vx[row * C::DS + sl];
+                }
             }
             return;
         }
@@ -195,13 +232,14 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
     auto request_k = [&](const Half (&hf)[2]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const unsigned char* krow = a.cache.k + (hf[h].row + m16) * C::RB + (C::RB < 64 ? 8 : 16) * q;
             if constexpr (E2M1) {
-                if constexpr (D == 128) kr[h][0] = *reinterpret_cast<const f32x4*>(krow);
-                else { const float2 w = *reinterpret_cast<const float2*>(krow); kr[h][0].x = w.x; kr[h][0].y = w.y; }
-                kx[h] = a.cache.kx[(hf[h].row + m16) * C::DS + (D == 128 ? q : q >> 1)];
+                const unsigned char* const rows = a.cache.k + hf[h].row * C::RB;
+                if constexpr (D == 128) kr[h][0] = load_from<f32x4>(rows, (uint32_t)(m16 * C::RB + 16 * q));
+                else { const u32x2 w = load_from<u32x2>(rows, (uint32_t)(m16 * C::RB + 8 * q)); kr[h][0] = __builtin_bit_cast(f32x4, u32x4{w.x, w.y, 0u, 0u}); }
+                kx[h] = load_from<uint8_t>(a.cache.kx + hf[h].row * C::DS, (uint32_t)(m16 * C::DS + (D == 128 ? q : q >> 1)));
                 continue;
             }
+            const unsigned char* krow = a.cache.k + (hf[h].row + m16) * C::RB + 16 * q;
 #pragma unroll
             for (int j = 0; j < C::KL; ++j) kr[h][j] = *reinterpret_cast<const f32x4*>(krow + 64 * j);
             if constexpr (E4M3) {
@@ -254,22 +292,34 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
 #pragma unroll
             for (int i = 0; i < C::NIV; ++i)
                 if constexpr (E2M1) {
-                    if (C::RPI * i + trow >= left || !(D == 128 ? hf[i].on : lane < 32 ? hf[0].on : hf[1].on)) { vr[i] = make_uint4(0u, 0u, 0u, 0u); vrx[i] = 127u; }
+                    if (C::RPI * i + trow >= left || !(D == 128 ? hf[i].on : lane < 32 ? hf[0].on : hf[1].on)) { vr[i] = u32x4{0u, 0u, 0u, 0u}; vrx[i] = 127u; }
                 } else
                 if (C::RPI * i + trow >= left || !hf[C::RPI * i / 16].on) *reinterpret_cast<f32x4*>(stage + i * 1024 + 16 * lane) = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         f32x4 s[NH][2];
 #pragma unroll
         for (int h = 0; h < NH; ++h) s[h][0] = s[h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (E2M1) {                                          // (both halves' products in turn: of one they wait for each other)
+#pragma unroll
+            for (int c = 0; c < C::KC; ++c) {
+                bf16x8 kf[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float w = kr[e][0][c];                       // (a bit cast of an element of a vector gives the first one's bits)
+                    kf[e] = bf16_of4(__builtin_bit_cast(uint32_t, w), scale_of_byte(kx[e], 0));
+                }
+#pragma unroll
+                for (int h = 0; h < NH; ++h)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) s[h][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[e], qf[h][c], s[h][e], 0, 0, 0);
+            }
+        } else
 #pragma unroll
         for (int e = 0; e < 2; ++e)
 #pragma unroll
             for (int c = 0; c < C::KC; ++c) {
                 bf16x8 kf;
-                if constexpr (E2M1) {
-                    const float w = kr[e][0][c];                       // (a bit cast of an element of a vector gives the first one's bits)
-                    kf = bf16_of4(__builtin_bit_cast(uint32_t, w), scale_of_byte(kx[e], 0));
-                } else if constexpr (E4M3) {
+                if constexpr (E4M3) {
                     const uint4 w = __builtin_bit_cast(uint4, kr[e][c / 2]);
                     kf = c % 2 ? bf16_of(w.z, w.w, scale_of_byte(kx[e], 0)) : bf16_of(w.x, w.y, scale_of_byte(kx[e], 0));
                 } else {
@@ -311,8 +361,12 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
                 if (!whole) x[r] = 16 * (r >> 2) + 4 * q + (r & 3) < left && hf[r >> 2].on ? x[r] : -INFINITY;
                 mx = fmaxf(mx, x[r]);
             }
-            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if constexpr (E2M1) {
+                mx = largest_of_rows(mx);
+            } else {
+                mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+                mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            }
             const float m_new = fmaxf(m_run[h], mx);
             const bool seen = m_new > -INFINITY;                       // (halves that are nowhere: perhaps no key yet)
             const float corr = seen ? fast_exp2((m_run[h] - m_new) * sc2) : 1.f;
@@ -335,6 +389,19 @@ __global__ __launch_bounds__(PG_THREADS, NH == 1 ? 4 : 2) void paged_kernel(Page
             pf[h] = f.v;
         }
         asm volatile("" : "+v"(vat));
+        if constexpr (E2M1 && !(NH == 2 && D == 64)) {                 // four of V's fragments are asked for before the first one is used (left to itself the compiler waits for each pair; of two blocks of heads of 64 it would hold more than 128 registers)
+#pragma unroll
+            for (int i0 = 0; i0 < C::DB; i0 += 4) {
+                Frag<T> vf[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { const unsigned char* va = stage + (vat ^ 32 * (i0 + i)); load_frag_tr(vf[i], va, va + 16 * C::SB); }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int h = 0; h < NH; ++h) oacc[h][i0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i].v, pf[h], oacc[h][i0 + i], 0, 0, 0);
+            }
+        } else
 #pragma unroll
         for (int i = 0; i < C::DB; ++i) {
             Frag<T> vf;
@@ -480,7 +547,7 @@ static size_t paged_smem_t(int G, int cuts, bool joins) {
 }
 template <int D, int NH, int TYPE>
 static hipError_t run_paged_t(const PagedArgs& a, int units, hipStream_t st) {
-    size_t smem = paged_smem_t<D, NH, TYPE>(a.G, paged_most_cuts(a.B, a.Hkv, a.most, a.whole), a.done != nullptr);
+    size_t smem = paged_smem_t<D, NH, TYPE>(a.G, paged_most_cuts(a.B, a.Hkv, a.most, TYPE == CACHE_E2M1), a.done != nullptr);
     if (a.B * a.Hkv <= PAGED_ALONE && smem <= 80 * 1024) smem = 80 * 1024 + 256;     // (a workgroup a compute unit, and none with two while another has none)
     hipLaunchKernelGGL((paged_kernel<D, NH, TYPE>), dim3(units), dim3(PG_THREADS), smem, st, a);
     if (!a.done) launch_paged_join(a, D, st);

@@ -27,7 +27,7 @@ __global__ __launch_bounds__(2 * D) void paged_join_kernel(PagedArgs a) {
     const int tid = threadIdx.x, sub = tid / LANES, dd = 2 * (tid % LANES);
     const int b = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, kvh = hq / a.G;
     PagedUnits w;
-    if (!w.find_head(a, b, kvh, tid & 63, a.whole) || w.cuts == 1) return;
+    if (!w.find_head(a, b, kvh, tid & 63) || w.cuts == 1) return;
     const float* src = a.part + ((int64_t)w.base * a.G + hq % a.G) * PS;
     const int64_t step = (int64_t)a.G * PS;
     float m = -INFINITY, o0 = 0.f, o1 = 0.f, l = 0.f;
@@ -67,24 +67,82 @@ __global__ __launch_bounds__(2 * D) void paged_join_kernel(PagedArgs a) {
     if (a.lse && dd == 0) a.lse[blockIdx.x] = l != 0.f ? (m * a.scale_log2e + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
+// The same for e2m1 pages, by what paged_kernel left of the heads (their parts need not be found again, which is most of a workgroup's time), WIDTH values of a query head a workgroup.  Of few rows a workgroup for a
+// whole one is the longest: one KV head of 128, 28129 positions, us by workgroups of 32 values / by paged_join_kernel: 32 query heads 14.5 / 16.3, 8 10.5 / 12.7; 65000, 32: 16.1 / 19.9.  Of many rows the workgroups
+// are too many: 8 sequences of 9000, 64 query heads of 64, by 32 values 15.5, by 64 14.0.
+constexpr int PAGED_JOIN_FEW = 256;
+template <int D, int WIDTH>
+__global__ __launch_bounds__(256) void paged4_join_kernel(PagedArgs a) {
+    constexpr int PS = D + 4, LANES = WIDTH / 2, SUBS = 256 / LANES, SHARES = D / WIDTH;
+    __shared__ float2 red[SUBS][LANES + 1];                    // of each subset: values, and behind them its normaliser
+    __shared__ float top[SUBS];
+    const int tid = threadIdx.x, sub = tid / LANES, at = tid % LANES, share = blockIdx.x % SHARES, row = blockIdx.x / SHARES;
+    const int b = row / a.Hq, hq = row - b * a.Hq, kvh = hq / a.G, dd = WIDTH * share + 2 * at;
+    const int2 parts = a.heads[b * a.Hkv + kvh];
+    if (parts.y == 1) return;
+    const float* src = a.part + ((int64_t)parts.x * a.G + hq % a.G) * PS;
+    const int64_t step = (int64_t)a.G * PS;
+    float m = -INFINITY, o0 = 0.f, o1 = 0.f, l = 0.f;
+    for (int s0 = sub; s0 < parts.y; s0 += SUBS * PG_BATCH) {
+        float2 x[PG_BATCH], ml[PG_BATCH];
+#pragma unroll
+        for (int e = 0; e < PG_BATCH; ++e) {
+            const int s = s0 + e * SUBS < parts.y ? s0 + e * SUBS : s0;
+            x[e] = *reinterpret_cast<const float2*>(src + s * step + dd);
+            ml[e] = *reinterpret_cast<const float2*>(src + s * step + D);
+        }
+        float m_new = m;
+#pragma unroll
+        for (int e = 0; e < PG_BATCH; ++e) m_new = fmaxf(m_new, ml[e].x);
+        const float corr = m > -INFINITY ? fast_exp2((m - m_new) * a.scale_log2e) : 0.f;
+        m = m_new; o0 *= corr; o1 *= corr; l *= corr;
+#pragma unroll
+        for (int e = 0; e < PG_BATCH; ++e) {
+            const bool is = s0 + e * SUBS < parts.y;           // (behind them part s0 once more: its infinities times 0 would be NaN)
+            const float wgt = ml[e].x > -INFINITY ? fast_exp2((ml[e].x - m) * a.scale_log2e) : 0.f;
+            o0 += is ? x[e].x * wgt : 0.f; o1 += is ? x[e].y * wgt : 0.f; l += is ? ml[e].y * wgt : 0.f;
+        }
+    }
+    red[sub][at] = make_float2(o0, o1);
+    if (at == 0) { red[sub][LANES] = make_float2(l, 0.f); top[sub] = m; }
+    __syncthreads();
+    if (sub > 0) return;
+    for (int u = 1; u < SUBS; ++u) m = fmaxf(m, top[u]);
+    o0 = o1 = l = 0.f;
+    for (int u = 0; u < SUBS; ++u) {
+        const float wgt = top[u] > -INFINITY ? fast_exp2((top[u] - m) * a.scale_log2e) : 0.f;
+        const float2 x = red[u][at];
+        o0 += x.x * wgt; o1 += x.y * wgt; l += red[u][LANES].x * wgt;
+    }
+    reinterpret_cast<uint32_t*>(reinterpret_cast<bf16_t*>(a.out) + (int64_t)row * D)[dd / 2] = (uint32_t)f2bf(l != 0.f ? o0 / l : 0.f) | ((uint32_t)f2bf(l != 0.f ? o1 / l : 0.f) << 16);
+    if (a.lse && dd == 0) a.lse[row] = l != 0.f ? (m * a.scale_log2e + log2f(l)) * 0.69314718055994531f : -INFINITY;
+}
+
 void launch_paged_join(const PagedArgs& a, int d, hipStream_t st) {
-    if (d == 128) hipLaunchKernelGGL((paged_join_kernel<128>), dim3(a.B * a.Hq), dim3(2 * 128), 0, st, a);
+    if (a.four) {
+        const int rows = a.B * a.Hq;
+        if (rows > PAGED_JOIN_FEW && d == 128) hipLaunchKernelGGL((paged4_join_kernel<128, 128>), dim3(rows), dim3(256), 0, st, a);
+        else if (rows > PAGED_JOIN_FEW) hipLaunchKernelGGL((paged4_join_kernel<64, 64>), dim3(rows), dim3(256), 0, st, a);
+        else if (d == 128) hipLaunchKernelGGL((paged4_join_kernel<128, 32>), dim3(rows * 4), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((paged4_join_kernel<64, 32>), dim3(rows * 2), dim3(256), 0, st, a);
+    } else if (d == 128) hipLaunchKernelGGL((paged_join_kernel<128>), dim3(a.B * a.Hq), dim3(2 * 128), 0, st, a);
     else hipLaunchKernelGGL((paged_join_kernel<64>), dim3(a.B * a.Hq), dim3(2 * 64), 0, st, a);
 }
 
 // A head's tiles are at most all there are, and a part no shorter than these by the slots: t / paged_length(..) <= slots / Hkv, whatever t is.
-int paged_most_cuts(int B, int Hkv, int64_t most, int whole) {
+int paged_most_cuts(int B, int Hkv, int64_t most, bool four) {
     const int64_t heads = (int64_t)B * Hkv, tiles = (most + PAGED_TILE - 1) / PAGED_TILE, by_work = (paged_slots(heads) + Hkv - 1) / Hkv;
-    const int64_t by_tiles = paged_cuts((int)tiles, paged_at_once(heads) ? PAGED_SHORTEST : PAGED_SHORTEST_MANY, whole);
+    const int least = paged_at_once(heads) ? paged_shortest(four) : PAGED_SHORTEST_MANY;
+    const int64_t by_tiles = paged_cuts((int)tiles, least, paged_whole(heads, least, 1, four));
     return (int)(by_work < by_tiles ? by_work : by_tiles);
 }
-int paged_units(int B, int Hkv, int64_t most, int whole) {
+int paged_units(int B, int Hkv, int64_t most, bool four) {
     // no more than the slots, or beside those the head that each part begins; and no more than all heads of the longest would be
-    const int64_t heads = (int64_t)B * Hkv, full = heads * paged_most_cuts(B, Hkv, most, whole), slots = paged_slots(heads) + (paged_at_once(heads) ? 0 : heads);
+    const int64_t heads = (int64_t)B * Hkv, full = heads * paged_most_cuts(B, Hkv, most, four), slots = paged_slots(heads) + (paged_at_once(heads) ? 0 : heads);
     return (int)(full < slots ? full : slots);
 }
 
-bool paged_joins(int B, int Hkv, int G, int64_t most, int whole) { return paged_most_cuts(B, Hkv, most, whole) * G <= PAGED_JOIN; }
+bool paged_joins(int B, int Hkv, int G, int64_t most, bool four) { return paged_most_cuts(B, Hkv, most, four) * G <= PAGED_JOIN; }
 
 hipError_t init_paged_kernels() {
     hipError_t e;

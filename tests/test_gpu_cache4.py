@@ -352,3 +352,32 @@ def test_heads_that_stay_whole(B, Hkv, Hq, n):
     out, lse, status = _attend(p, q, table, lens, times=3)
     assert status == 0
     _check(p, q, table, lens, out, lse)
+
+
+@pytest.mark.parametrize("B,Hkv,Hq,d,n", [(16, 8, 8, 64, 1152), (16, 8, 8, 64, 1153), (66, 1, 2, 64, 1153), (64, 1, 2, 128, 512), (64, 1, 2, 128, 513), (40, 4, 8, 64, 2304), (40, 4, 4, 128, 2305),
+                                         (70, 2, 2, 64, 2304), (70, 2, 40, 64, 2305)])
+def test_heads_that_are_cut_from_a_length_on(B, Hkv, Hq, d, n):
+    """Sequences at either side of the lengths from which heads are cut into parts, where the others are short."""
+    rng = np.random.default_rng(B + n)
+    lens = [int(x) for x in rng.integers(0, 40, B)]
+    lens[3], lens[B - 1], lens[B // 2] = n, n - 1, 0
+    pages = sum(-(-x // 64) for x in lens)
+    p = p4.pool(rng, pages, Hkv, 64, d)
+    q, table = pu.rnd(rng, B, Hq, d, scale=1.5), pu.table_for(rng, lens, 64, pages)
+    print("paged4 cut", B, Hkv, Hq, d, n, flush=True)
+    out, lse, status = _attend(p, q, table, lens, times=3)
+    assert status == 0
+    _check(p, q, table, lens, out, lse)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,d", [([28129], 32, 1, 128), ([9001], 32, 1, 64), ([0, 20000, 1, 700], 32, 1, 128), ([12000, 0, 511, 513, 14001], 40, 2, 64), ([1] * 30 + [16384] + [0] * 10, 24, 1, 128)])
+def test_parts_that_a_launch_more_puts_together(lens, Hq, Hkv, d):
+    """Many parts of many query heads, beside sequences of one part and of none, over unlike calls on the same workspace."""
+    rng = np.random.default_rng(sum(lens) + d)
+    pages = sum(-(-x // 64) for x in lens)
+    p = p4.pool(rng, pages, Hkv, 64, d)
+    q, table = pu.rnd(rng, len(lens), Hq, d, scale=1.5), pu.table_for(rng, lens, 64, pages)
+    print("paged4 joined", lens[:5], Hq, Hkv, d, flush=True)
+    out, lse, status = _attend(p, q, table, lens, times=3)
+    assert status == 0
+    _check(p, q, table, lens, out, lse)
