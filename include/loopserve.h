@@ -350,7 +350,7 @@ int ls_cache_read(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, con
  *   (LS_STAT_PAGE_RANGE).  Sequences that shrink give the pages that they no longer need to the back of the ring, in order, for calls to come; their table entries stay, and mean nothing.
  *   A length outside [0, max_pages * page] stays as it is, likewise a ring that does not have that many (it holds no page then, and pages that it has no room for are lost; LS_STAT_PAGE_RANGE).
  *   Pages that several sequences share are each sequence's here: give them back once.
- * Outputs (device memory; new_len and new_state may be len and state themselves):
+ * Outputs (device memory; new_len and new_state may be len and state themselves, and no output overlaps anything else):
  *   new_len [B], new_state [2], table, free_pages
  *   starts [B+1] int32: the rows of the step, packed: sequence b adds rows starts[b] .. starts[b+1] - 1, add[b] of them where that is positive (also where it
  *        does not grow).  A sequence whose rows go beyond n_hat has none and does not grow, like all behind it (LS_STAT_STARTS).

@@ -744,9 +744,14 @@ Wrong check_resize(const ls_shape* s, const ls_cache* cache, const int32_t* free
         if (!aligned4(p)) return {LS_EINVAL, "misaligned index tensor"};
     if (reinterpret_cast<uintptr_t>(slots) & 7u) return {LS_EINVAL, "misaligned index tensor"};
     if (overlap(state, new_state, 2) || overlap(len, new_len, s->B)) return {LS_EINVAL, "an output overlaps its input without being it"};
+    if (add == new_len || overlap(add, new_len, s->B)) return {LS_EINVAL, "new_len overlaps add"};
     return FINE;
 }
 
+// Whether rows that begin where others do are not those
+bool elsewhere(const ls_rows* a, const ls_rows* b, int64_t seqs, int64_t rows, int64_t heads) {
+    return a->data == b->data && ((seqs > 1 && a->seq != b->seq) || (rows > 1 && a->row != b->row) || (heads > 1 && a->head != b->head));
+}
 Wrong check_rotate(const ls_shape* s, const ls_rotation* r, const ls_rows* q, const ls_rows* k, const int32_t* positions, const ls_rows* q_out, const ls_rows* k_out,
                    const ls_cache* cache, const ls_rows* v, const int64_t* slots) {
     Wrong w = check_heads(s, true);
@@ -765,6 +770,7 @@ Wrong check_rotate(const ls_shape* s, const ls_rotation* r, const ls_rows* q, co
     if ((w = check_rows(q, s->dtype, s->d, s->B, s->n_hat, s->Hq, false)).code || (w = check_rows(k, s->dtype, s->d, s->B, s->n_hat, s->Hkv, false)).code ||
         (w = check_rows(q_out, s->dtype, s->d, s->B, s->n_hat, s->Hq, true)).code) return w;
     if (k_out && (w = check_rows(k_out, s->dtype, s->d, s->B, s->n_hat, s->Hkv, true)).code) return w;
+    if (elsewhere(q, q_out, s->B, s->n_hat, s->Hq) || (k_out && elsewhere(k, k_out, s->B, s->n_hat, s->Hkv))) return {LS_EINVAL, "rows in place need the strides that they have"};
     return v ? check_rows(v, s->dtype, s->d, s->B, s->n_hat, s->Hkv, false) : FINE;
 }
 

@@ -26,7 +26,7 @@ __device__ __forceinline__ uint32_t row_upto(uint32_t x) {
     return (uint32_t)s;
 }
 
-constexpr int RESIZE_WAVES = 16, RESIZE_THREADS = 64 * RESIZE_WAVES, RESIZE_ALONE = 4 * RESIZE_THREADS;
+constexpr int RESIZE_WAVES = 16, RESIZE_THREADS = 64 * RESIZE_WAVES, RESIZE_ALONE = 8 * RESIZE_THREADS;
 
 template <bool PACKED>
 __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a) {
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
 hipError_t run_resize(ResizeArgs a, hipStream_t st) {
     const bool in_place = a.new_len == a.len || a.new_state == a.state;
     const int64_t rows = a.starts ? a.n_rows : (int64_t)a.B * a.n_rows, groups = (rows + RESIZE_THREADS - 1) / RESIZE_THREADS;
-    // In place one workgroup does it alone up to here: a launch more takes 4 us.
+    // In place one workgroup does it alone up to here: a launch more takes 3 us.  (64 sequences that grow and shrink in turn, us, alone / in two launches: 2048 rows 5.3 / 8.5, 4096 5.9 / 8.7, 8192 7.8 / 8.0 to 9.0, 16384 12.3 / 8.9.)
     const int grid = in_place && rows <= RESIZE_ALONE ? 1 : groups < 256 ? (int)groups : 256;
     a.bulk = 1;
     a.finish = grid == 1 || !in_place;

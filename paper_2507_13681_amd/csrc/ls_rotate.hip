@@ -16,7 +16,7 @@ namespace ls {
 constexpr int ROTATE_THREADS = 256;
 constexpr int NO_PAGES = -1;
 constexpr int rotate_rows(int d) { return 4096 / d; }      // of a workgroup, at most
-constexpr int ROTATE_FEW = 1024;
+constexpr int ROTATE_FEW = 1280;
 
 // Sum over the L (4 or 8) neighbouring lanes of a row, in every lane
 template <int L>
@@ -202,7 +202,8 @@ static hipError_t run_rotate_t(RotateArgs a, hipStream_t st) {
     constexpr int GROUPS = ROTATE_THREADS / (D / 16);
     const int64_t rows = (int64_t)a.B * a.n_hat;
     a.heads = a.Hq + (TYPE == NO_PAGES ? 1 : 2) * a.Hkv;
-    // Three to six items a group where there are rows enough, as many as leave the fewest groups idle in the end; else one.
+    // Three to six items a group where there are rows enough, as many as leave the fewest groups idle in the end; else one.  (32 and 8 heads of 128, us, one / more: into rows 500 rows 5.1 / 7.5,
+    // 1000 7.8 / 9.4, 2500 13.9 / 12.2, 8000 48.9 / 38.4; into rows and pages 500 5.4 / 6.9, 800 7.9 / 8.1, 1000 8.8 / 8.6, 1500 10.9 / 9.7, 8000 56.2 / 47.4.)
     const bool few = rows * a.heads <= (int64_t)ROTATE_FEW * GROUPS;
     const int most = few ? GROUPS : 6 * GROUPS;
     a.chunk = a.heads < most ? a.heads : most;

@@ -17,6 +17,8 @@ RESIZE = [
     (dict(shape=dict(n_hat=2147483000)), 0), (dict(starts=None, shape=dict(n_hat=2147483000)), ESHAPE), (dict(starts=None, shape=dict(n_hat=1073741500)), 0),
 ]
 
+RESIZE += [(dict(add=HERE + 4096), EINVAL), (dict(add=HERE + 4100), EINVAL), (dict(add=HERE + 4092), EINVAL), (dict(add=HERE + 4104), 0), (dict(add=HERE + 4096, new_len=HERE + 8192), 0)]
+
 
 @pytest.mark.parametrize("change,want", RESIZE)
 def test_refusals(lib, change, want):  # noqa: F811

@@ -19,10 +19,17 @@ ROTATE = [
     (dict(rot=dict(freq=None)), EINVAL), (dict(rot=dict(freq=HERE + 4)), EINVAL), (dict(rot=dict(k_weight=HERE + 8)), EINVAL), (dict(rot=dict(pairs=2)), EINVAL),
     (dict(rot=dict(dims=8)), ESHAPE), (dict(rot=dict(dims=144)), ESHAPE), (dict(rot=dict(dims=-16)), ESHAPE), (dict(rot=dict(eps=-1e-9)), EINVAL), (dict(rot=dict(eps=NAN)), EINVAL),
     (dict(rot=dict(eps=INF)), EINVAL), (dict(positions=HERE + 2), EINVAL), (dict(slots=HERE + 4), EINVAL), (dict(q=None), EINVAL), (dict(k=None), EINVAL), (dict(q_out=None), EINVAL),
-    (dict(q_out=_rows(row=512, head=128, seq=102400)), ESHAPE), (dict(k_out=_rows(row=0, seq=51200)), ESHAPE), (dict(k=_rows(row=0, head=0)), 0), (dict(v=_rows(data=HERE + 8)), EINVAL),
+    (dict(q_out=_rows(row=512, head=128, seq=102400)), ESHAPE), (dict(k_out=_rows(row=0, seq=51200)), ESHAPE), (dict(k=_rows(row=0, head=0, data=HERE + (1 << 24))), 0), (dict(v=_rows(data=HERE + 8)), EINVAL),
     (dict(shape=dict(d=96)), ESHAPE), (dict(shape=dict(Hq=6)), ESHAPE), (dict(shape=dict(n_hat=0)), ESHAPE), (dict(shape=dict(n_hat=2 ** 31)), ESHAPE), (dict(shape=dict(n_hat=2 ** 62)), ESHAPE),
     (dict(shape=dict(n_hat=2147483000)), ESHAPE), (dict(shape=dict(B=0)), ESHAPE), (dict(shape=dict(B=9000)), ESHAPE), (dict(cache=dict(page=24)), ESHAPE), (dict(cache=dict(Hkv=2)), ESHAPE),
     (dict(cache=dict(type=2)), EINVAL), (dict(cache=dict(type=4)), 0), (dict(cache=dict(type=0, k_exp=None, v_exp=None)), 0), (dict(cache=dict(type=4, v_exp=None)), EINVAL), (dict(cache=dict(pages=0)), ESHAPE),
+]
+
+AT = HERE + (1 << 24)
+ROTATE += [     # in place, with the strides of the rows that are read and with others; of a row or a head the stride is nobody's
+    (dict(q=_rows(row=1024, seq=102400, data=AT), q_out=_rows(row=1024, seq=102400, data=AT)), 0), (dict(q=_rows(row=2048, seq=204800, data=AT), q_out=_rows(row=1024, seq=102400, data=AT)), EINVAL),
+    (dict(q=_rows(row=1024, seq=204800, data=AT), q_out=_rows(row=1024, seq=102400, data=AT)), EINVAL), (dict(k=_rows(seq=51200, data=AT), k_out=_rows(seq=51200, data=AT)), 0),
+    (dict(k=_rows(row=0, head=0, data=AT), k_out=_rows(seq=51200, data=AT)), EINVAL), (dict(k=_rows(row=2048, seq=51200, data=AT), k_out=_rows(seq=51200, data=AT), shape=dict(n_hat=1)), 0),
 ]
 
 
