@@ -3,7 +3,7 @@
 //
 // The step reads every K and V row once and does 4 d FLOP per (query head, key): it is bound by HBM bandwidth, at small sizes by latency.
 // The query heads of a KV head are the columns of 16x16x32 products (NH blocks of 16), so that the rows are read once for all of them.
-//   Work.  What there is to do follows from the lengths, which only the device knows: every wave adds them up, cuts each KV head's 32-key tiles into parts of about
+//   Work.  What there is to do follows from the lengths, which only the device knows: every wave (of e2m1 pages one of a workgroup) adds them up, cuts each KV head's 32-key tiles into parts of about
 //   equal length (PagedLength) and finds the part that its workgroup has, so a batch of one long and many short sequences fills the chip as one of equals does.
 //   A part.  The waves of a workgroup take its tiles in turn.  S^T = K Q^T with K fragments straight from global memory, online softmax per head in a lane,
 //   P -> bf16, O^T += V^T P^T with the V^T fragments read transposed from a wave-private, swizzled LDS copy of the 32 V rows that a global -> LDS transfer filled.

@@ -6,7 +6,8 @@
 // workgroups evenly, however unevenly the sequences have them, and which sequence one is of is found by bisecting the sums in LDS.
 // Nobody waits for anybody: pages that are taken are read where those that are given back in the same call are not written, table entries that are read (of positions that were there) are none of those
 // that are written, and where lengths or the ring's state are updated in place by more than one workgroup, a launch of one more does that behind the others.
-// Bound by its launch and a chain of dependent loads (lengths, then pages, then rows).
+// Bound by its launch and a chain of dependent loads (lengths, then pages, then rows), and of many sequences by the sums.  A decode step in place, us: 4 sequences 3.9, 256 4.6, 1024 5.6, 4096 17, 65535 292 (they
+// come 1024 at a time); sixteen sequences that grow by 23900 rows in all 4.7; 512 by 1.04 million rows 10.7 (13 MB: 2.5 of them).
 #include "ls_rows.h"
 
 namespace ls {
