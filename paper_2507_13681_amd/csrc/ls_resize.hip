@@ -57,7 +57,7 @@ __global__ __launch_bounds__(RESIZE_THREADS, 8) void resize_kernel(ResizeArgs a)
         int64_t before, sum;
         if (__ballot(w >> 28 != 0) == 0ull) {
             const uint32_t s = row_upto((uint32_t)w);
-            before = wv ? __builtin_amdgcn_readlane((int)s, wv - 1) : 0;
+            before = wv ? (uint32_t)__builtin_amdgcn_readlane((int)s, wv - 1) : 0u;              // (up to 2^32: lanes are read as int, which would be negative here)
             sum = (uint32_t)__builtin_amdgcn_readlane((int)s, WAVES - 1);
         } else {
             const uint32_t lo = row_upto((uint32_t)w & 0xFFFFFFu), hi = row_upto((uint32_t)(w >> 24));

@@ -208,6 +208,51 @@ def test_sums_beyond_32_bits(in_place):
     assert status == STARTS and s.host["lens"][11] == 40 and s.host["lens"][13] == 400
 
 
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("B,each,max_pages", [(1024, 2300000, 8), (1024, 4000000, 15625), (1024, 4194303, 16384), (2500, 4000000, 15625), (2500, 4194303, 8)])
+def test_sums_between_31_and_32_bits(B, each, max_pages, in_place):
+    """Sequences whose rows are few for 64 of them (less than 2^28) and more than 2^31 for a thousand; a table in which they would fit, or not.  The last one asks for a row."""
+    s = Server(B, 64, 256, max_pages, in_place)
+    add = np.full(B, each, np.int64)
+    add[:4], add[B - 1] = (700, 0, 1, 257), 1
+    print("resize sums of 32 bits", B, each, max_pages, in_place, flush=True)
+    _, status = s.step(add, n_rows=9001)
+    assert status == STARTS and list(s.host["lens"]) == [700, 0, 1, 257] + [0] * (B - 4)
+    _, status = s.step(add, n_rows=9001, padded=True)
+    assert status == STARTS and list(s.host["lens"]) == [1400, 0, 2, 514] + [0] * (B - 5) + [1]
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+def test_two_billion_rows(in_place):
+    """Starts of as many rows as a call can have, without positions and slots: 500 sequences have room, and three find pages."""
+    B, each, page, max_pages, pages = 1024, 4000000, 256, 15625, 3 * 15625 + 100
+    s = Server(B, pages, page, max_pages, in_place)
+    d, starts = s.dev, _i32([77] * (B + 1))
+    table = d["table"].clone()
+    new = {} if in_place else dict(new_state=_i32([77, 77]), new_lens=_i32([77] * B))
+    print("resize two billion rows", in_place, flush=True)
+    s.ctx.ls_cache_resize(binding.make_shape(B, 1, 1, 64, 1, 2000000000, 1, "bf16"), s.cache, d["free"], d["state"], _i32([each] * B), d["lens"], d["table"], starts=starts, **new)
+    assert s.ctx.ls_poll_status() == OUT | STARTS
+    table[:3] = torch.arange(3 * max_pages, dtype=torch.int32, device="cuda").view(3, max_pages)
+    assert torch.equal(starts.cpu().long(), torch.arange(B + 1).clamp(max=500) * each)
+    assert new.get("new_lens", d["lens"]).tolist() == [each] * 3 + [0] * (B - 3) and new.get("new_state", d["state"]).tolist() == [3 * max_pages, 100]
+    assert torch.equal(d["table"], table) and torch.equal(d["free"], torch.arange(pages, dtype=torch.int32, device="cuda"))
+
+
+def test_pages_given_back_beyond_31_bits():
+    """A thousand sequences that end, of more pages than 2^31 in all: the ring takes those that it has room for, the first ones in order."""
+    B, max_pages, page, pages = 1024, 2200000, 16, 50
+    s = Server(1, pages, page, 4)
+    print("resize pages given back beyond 31 bits", flush=True)
+    table = torch.full((B, max_pages), 7, dtype=torch.int32, device="cuda")      # 9 GB; entries behind the room of the ring are not looked at
+    table[0, :100] = torch.arange(100, 200, dtype=torch.int32, device="cuda")
+    free, state, lens, starts = _i32(list(range(pages))), _i32([45, 20]), _i32([page * max_pages] * B), _i32([77] * (B + 1))
+    s.ctx.ls_cache_resize(binding.make_shape(B, 1, 1, 64, 1, 10, 1, "bf16"), s.cache, free, state, _i32([-2147483648] * B), lens, table, starts=starts)
+    assert s.ctx.ls_poll_status() == RANGE
+    assert lens.tolist() == [0] * B and state.tolist() == [45, 50] and starts.tolist() == [0] * (B + 1)
+    assert free.tolist() == list(range(15)) + list(range(100, 130)) + list(range(45, 50))
+
+
 def test_as_many_sequences_as_there_can_be():
     B = 65535
     s = Server(B, B, 16, 1)
