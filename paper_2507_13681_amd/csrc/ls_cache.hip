@@ -30,21 +30,7 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
     const int64_t row0 = (a.group0 + blockIdx.x) * ROWS;
     const bool first = row0 == 0 && blockIdx.y == 0;
     int b = -1, i = 0;
-    int64_t at = row0 + slot, seq = 0;                     // the row, and that of the tensor it is
-    const bool is = at < (a.starts ? 1 : (int64_t)a.B) * a.n_hat;
-    if (!a.starts) {
-        seq = is ? at / a.n_hat : 0;
-        at -= seq * a.n_hat;
-    }
-    const int h0 = blockIdx.y * a.heads, h1 = h0 + a.heads < a.cache.Hkv ? h0 + a.heads : a.cache.Hkv;
-    unsigned char* const rows[2] = {a.k.data + (seq * a.k.seq + at * a.k.row + 8 * part) * SRC, a.v.data + (seq * a.v.seq + at * a.v.row + 8 * part) * SRC};
-    const int64_t step[2] = {a.k.head * SRC, a.v.head * SRC};
-    Eight<T> ahead[4];                                     // rows that are written are asked for before it is known where they go
-    auto ask = [&](int h) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) ahead[j].load(rows[j & 1] + (h + j / 2) * step[j & 1]);
-    };
-    if (WRITE && is && h0 + 2 <= h1) ask(h0);
+    int64_t at = row0 + slot;                              // the row, and that of the tensor it is
     if (a.starts) {
         // Each sequence lays claim to its rows among these, up to the first one whose starts are none.
         if (tid < ROWS) seq_s[tid] = -1;
@@ -63,18 +49,29 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
         __syncthreads();
         b = seq_s[slot];
         if (b >= 0) i = (int)(at - a.starts[b]);
-    } else if (is) {
-        b = (int)seq;
-        i = (int)at;
+    } else if (at < (int64_t)a.B * a.n_hat) {
+        b = (int)(at / a.n_hat);
+        i = (int)(at - (int64_t)b * a.n_hat);
+        at = i;
         if (a.count && i >= a.count[b]) b = -1;
     }
-    int page = -1;
-    int64_t p = 0;
-    if (b >= 0) {
-        p = (a.pos ? (int64_t)a.pos[b] : 0) + i;
-        page = page_of(a.cache, b, p);
-        if (page < 0 && part == 0 && blockIdx.y == 0) atomicOr(a.status, STAT_PAGE_RANGE);
-    }
+    if (b < 0) return;
+    const int h0 = blockIdx.y * a.heads, h1 = h0 + a.heads < a.cache.Hkv ? h0 + a.heads : a.cache.Hkv;
+    const int64_t seq = a.starts ? 0 : b;
+    unsigned char* const rows[2] = {a.k.data + (seq * a.k.seq + at * a.k.row + 8 * part) * SRC, a.v.data + (seq * a.v.seq + at * a.v.row + 8 * part) * SRC};
+    const int64_t step[2] = {a.k.head * SRC, a.v.head * SRC};
+    // Rows that are written go by here four at a time; the first of them into bf16 pages are asked for before it is known where they go.  (Us, with / without: 10923 rows of 8 heads of 128 18.1 / 18.7, 24 sequences of 0 to 512 padded
+    // 9.5 / 10.1; codes have more to do behind their loads and gain nothing: e4m3 15.0 / 14.7, 11.1 / 10.6, e2m1 13.5 / 13.4, 10.0 / 9.7.)  Rows that are none are not read: a padded batch is mostly those.
+    constexpr bool AHEAD = WRITE && TYPE == CACHE_BF16;
+    Eight<T> ahead[4];
+    auto ask = [&](int h) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ahead[j].load(rows[j & 1] + (h + j / 2) * step[j & 1]);
+    };
+    if (AHEAD && h0 + 2 <= h1) ask(h0);
+    const int64_t p = (a.pos ? (int64_t)a.pos[b] : 0) + i;
+    const int page = page_of(a.cache, b, p);
+    if (page < 0 && part == 0 && blockIdx.y == 0) atomicOr(a.status, STAT_PAGE_RANGE);
     if (page < 0) return;
     const int64_t place = ((int64_t)page * a.cache.Hkv << a.cache.page_log) + (p & ((1 << a.cache.page_log) - 1));       // of head 0, in rows
     unsigned char* const pool[2] = {a.cache.k, a.cache.v};
@@ -86,7 +83,7 @@ __global__ __launch_bounds__(MOVE_THREADS) void move_kernel(MoveArgs a) {
     if constexpr (WRITE) {
         int h = h0;
         for (; h + 2 <= h1; h += 2) {                      // four rows in flight
-            if (h != h0) ask(h);
+            if (!AHEAD || h != h0) ask(h);
 #pragma unroll
             for (int j = 0; j < 4; ++j) put(ahead[j], h + j / 2, j & 1);
         }
