@@ -402,8 +402,8 @@ int ls_norm_rotate(ls_ctx* ctx, const ls_shape* shape, const ls_rotation* rotati
  * Outputs:
  *   out [B,Hq,d] in dtype; all zeros where there is no key, NaN (and so the lse) where a logit is
  *   lse [B,Hq] fp32 or NULL: natural log of the softmax denominator (-inf when there is no key)
- * Workspace: ls_paged_workspace_bytes (0 for an invalid shape).  What this header says of calls of ls_decode_attend that overlap holds for
- * these too: they share its counters.
+ * Workspace: ls_paged_workspace_bytes (0 for an invalid shape), of which LS_CACHE_E2M1 pages alone need the last 8 bytes a sequence and KV head (rounded up to 256 in all).
+ * What this header says of calls of ls_decode_attend that overlap holds for these too: they share its counters.
  */
 int ls_paged_attend(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, const void* q,
                     const int32_t* table, int32_t max_pages, const int32_t* len, void* out, float* lse, void* hip_stream);

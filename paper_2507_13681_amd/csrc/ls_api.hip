@@ -815,9 +815,9 @@ ls::PackedCut packed_cut(const ls_shape* s, bool packed, size_t room) {
     return ls::packed_cut(s->B, packed, s->n, s->n_hat, s->Hkv, s->Hq / s->Hkv, s->dtype, s->d, (int64_t)(room / ls::prefill_slot_bytes(s->d)));
 }
 size_t paged_part_bytes(const ls_shape* s) { return up((size_t)ls::paged_units(s->B, s->Hkv, s->n) * (s->Hq / s->Hkv) * ls::decode_part_floats(s->d) * 4); }
-size_t paged_bytes(const ls_shape* s) {                    // parts' results, and where each head's are
+size_t paged_bytes(const ls_shape* s, bool four) {         // parts' results, and of e2m1 pages where each head's are
     if (ls::paged_most_cuts(s->B, s->Hkv, s->n) == 1) return 0;
-    return paged_part_bytes(s) + up((size_t)s->B * s->Hkv * sizeof(int2));
+    return paged_part_bytes(s) + (four ? up((size_t)s->B * s->Hkv * sizeof(int2)) : 0);
 }
 }  // namespace
 
@@ -891,19 +891,19 @@ int ls_packed_prefill(ls_ctx* c, const ls_shape* s, const ls_rows* q, const ls_r
     return LS_OK;
 }
 
-size_t ls_paged_workspace_bytes(const ls_shape* s) { return check_paged_shape(s).code ? 0 : paged_bytes(s) + ALIGN; }
+size_t ls_paged_workspace_bytes(const ls_shape* s) { return check_paged_shape(s).code ? 0 : paged_bytes(s, true) + ALIGN; }
 
 int ls_paged_attend(ls_ctx* c, const ls_shape* s, const ls_cache* cache, const void* q, const int32_t* table, int32_t max_pages,
                     const int32_t* len, void* out, float* lse, void* stream) {
     if (!c) return LS_EINVAL;
     if (const Wrong w = check_paged(s, cache, q, table, max_pages, len, out, lse); w.code) return fail(c, w.code, "ls_paged_attend: %s", w.what);
-    if (paged_bytes(s) > c->ws_bytes) return fail(c, LS_EWORKSPACE, "ls_paged_attend: workspace of %zu bytes is too small", c->ws_bytes);
+    if (paged_bytes(s, cache->type == LS_CACHE_E2M1) > c->ws_bytes) return fail(c, LS_EWORKSPACE, "ls_paged_attend: workspace of %zu bytes is too small", c->ws_bytes);
     ls::PagedArgs a{};
     a.cache = cache_args(cache, table, max_pages);
     a.q = q; a.len = len; a.out = out; a.lse = lse; a.part = reinterpret_cast<float*>(c->ws);
     a.B = s->B; a.Hq = s->Hq; a.Hkv = s->Hkv; a.G = s->Hq / s->Hkv; a.most = s->n; a.scale_log2e = scale_log2e(s); a.status = c->status;
     a.four = cache->type == LS_CACHE_E2M1;
-    a.heads = reinterpret_cast<int2*>(c->ws + paged_part_bytes(s));
+    a.heads = a.four ? reinterpret_cast<int2*>(c->ws + paged_part_bytes(s)) : nullptr;
     const bool joins = ls::paged_joins(s->B, s->Hkv, a.G, s->n, a.four), counts = joins && ls::paged_most_cuts(s->B, s->Hkv, s->n, a.four) > 1;
     a.done = joins ? decode_set(c, c->decode_calls) : nullptr;
     a.done_clear = decode_set(c, c->decode_calls + 2);

@@ -1,4 +1,6 @@
 """Pages of 4-bit floats: stored bits, the way back, attention over them in 64 bits, and what is left out."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -381,3 +383,31 @@ def test_parts_that_a_launch_more_puts_together(lens, Hq, Hkv, d):
     out, lse, status = _attend(p, q, table, lens, times=3)
     assert status == 0
     _check(p, q, table, lens, out, lse)
+
+
+def test_workspace_by_the_type_of_the_pages():
+    """Where each head's parts are is kept for 4-bit pages alone: the others take a workspace that has the parts' results and no more, and nothing is written beyond it."""
+    B, Hq, Hkv, d, n, page = 16, 32, 8, 64, 3000, 64
+    rng = np.random.default_rng(11)
+    lens, q = [n] + [int(x) for x in rng.integers(0, n, B - 1)], pu.rnd(rng, B, Hq, d)
+    shape = binding.make_shape(B, Hq, Hkv, d, n, 1, 1, "bf16")
+    cuts, most = (C.c_int32 * B)(), C.c_int32()
+    units = binding.load_library().ls_debug_paged_cuts(C.byref(shape), (C.c_int32 * B)(*lens), cuts, C.byref(most))
+    parts = -(-units * (Hq // Hkv) * (d + 4) * 4 // 256) * 256
+    assert most.value > 1 and parts + 8 * B * Hkv <= binding.paged_workspace_bytes(shape)
+    pages = sum(-(-x // page) for x in lens)
+    table = pu.table_for(rng, lens, page, pages)
+    for kind in ("bf16", "e4m3", "e2m1"):
+        p = p4.pool(rng, pages, Hkv, page, d) if kind == "e2m1" else pu.pool(rng, pages, Hkv, page, d, kind)
+        cache, got = _cache(p), []
+        for bytes_ in (binding.paged_workspace_bytes(shape), parts, parts - 256):
+            print("paged workspace", kind, bytes_, flush=True)
+            ctx, out = binding.Context(workspace=bytes_), torch.full(q.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+            call = lambda: ctx.ls_paged_attend(shape, cache, q.cuda(), table.cuda(), _i32(lens), out)
+            if bytes_ < (parts + 8 * B * Hkv if kind == "e2m1" else parts):
+                with pytest.raises(binding.LoopServeError):
+                    call()
+                continue
+            call()
+            got.append(out.cpu())
+        assert all(torch.equal(x, got[0]) for x in got) and not got[0].isnan().any() and len(got) == (1 if kind == "e2m1" else 2)
