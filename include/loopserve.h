@@ -340,8 +340,9 @@ int ls_cache_read(ls_ctx* ctx, const ls_shape* shape, const ls_cache* cache, con
  * ls_cache_resize -- sequences that grow and shrink: pages for them from a ring of free ones and back to it, and for the rows that a step adds what the other calls
  * take.  Once a step, for all layers whose pools are alike (they share the table).
  *
- *   shape: B sequences, Hkv and d of the cache; n_hat >= 1: rows that positions and slots have room for, in all or of each sequence.  Hq, n, w, dtype, scale are ignored.
- *   cache: of which `page` and `pages` are used
+ *   shape: B sequences, Hkv and d of the cache, B * Hkv <= 65535 (as every call on pages has it), a dtype; n_hat >= 1: rows that positions and slots have room for, in all or of each
+ *        sequence.  Hq, n, w, scale are ignored, and it makes no difference which dtype it is.
+ *   cache: of which `page` and `pages` are used; it has to be one that the other calls take (its type, sizes and addresses are checked as theirs)
  *   free_pages [pages] int32, state [2] int32: a ring.  The numbers of the free pages are its `state[1]` entries from entry state[0] on, and behind the last entry comes
  *        the first.  (In the beginning: 0 .. pages - 1, and {0, pages}.)
  *   len [B] int32: positions that each sequence has; add [B] int32: by how many it grows, or, negative, shrinks (to none at least)

@@ -19,6 +19,11 @@ RESIZE = [
 
 RESIZE += [(dict(add=HERE + 4096), EINVAL), (dict(add=HERE + 4100), EINVAL), (dict(add=HERE + 4092), EINVAL), (dict(add=HERE + 4104), 0), (dict(add=HERE + 4096, new_len=HERE + 8192), 0)]
 
+# the cache and the shape are checked as the other calls on pages check theirs, although its page and its number of pages are all that is used
+RESIZE += [(dict(cache=dict(k=None)), EINVAL), (dict(cache=dict(v=HERE + 8)), EINVAL), (dict(cache=dict(k_exp=None)), EINVAL), (dict(cache=dict(k_exp=None, v_exp=None, type=0)), 0),
+           (dict(cache=dict(Hkv=8), shape=dict(Hkv=8, B=8191), add=16 * HERE), 0), (dict(cache=dict(Hkv=8), shape=dict(Hkv=8, B=8192), add=16 * HERE), ESHAPE), (dict(cache=dict(Hkv=1), shape=dict(Hkv=1, B=65535), add=16 * HERE), 0),
+           (dict(shape=dict(dtype="f32")), 0), (dict(cache=dict(d=64)), ESHAPE)]
+
 
 @pytest.mark.parametrize("change,want", RESIZE)
 def test_refusals(lib, change, want):  # noqa: F811
