@@ -2,7 +2,7 @@
 //
 // Bound by memory: each row is read and written once, and of each position the table's entry.  8 KV heads of 128, e4m3, us: 32768 bf16 rows written 43 (4.7 TB/s, read and written), four caches of
 // 16384 read back 79 (5.1 TB/s; a copy of 1 GiB reaches 5.15); one row of each of four sequences written 4.6, where an empty launch is 2.6.
-// e2m1: 10923 rows written 18.6, or 15 where they are on the chip (57 MB: 11 at a copy's rate), 32768 read back 37.4 (kernel 33, 5.1 TB/s).
+// e2m1: 10923 rows written 17.2, or 13.1 where they are on the chip, or 22 (kernel) behind a call that wrote 134 MB (57 MB: 11 at a copy's rate), 32768 read back 37.6 (kernel 33, 5.1 TB/s).
 #include "ls_rows.h"
 
 namespace ls {

@@ -242,7 +242,7 @@ constexpr int PAGED_WHOLE = 16;
 constexpr int PAGED_SHORTEST = 4, PAGED_SHORTEST_MANY = 32;                          // tiles of a part at least; of that many heads
 __host__ __device__ inline int paged_cuts(int tiles, int length, int whole = PAGED_WHOLE) { return tiles <= whole ? 1 : (int)(((uint32_t)tiles + (uint32_t)length - 1) / (uint32_t)length); }
 // .. of e2m1 pages a tile a wave: a part writes 4 (d + 4) bytes of each query head, which two of these tiles read.  (8 / 4, us: one sequence of 131072, 8 KV heads 35.0 / 36.2; 64 of 0 to 1500, 2 KV heads of 32
-// query heads each 18.4 / 26.1; three drawn batches 9.2 / 10.6, 11.9 / 13.2, 12.2 / 16.0.)
+// query heads each 18.4 / 26.1.)
 __host__ __device__ inline int paged_shortest(bool four) { return four ? 8 : PAGED_SHORTEST; }
 // .. and of more than PAGED_ALONE heads stay whole by how long parts are: e2m1 tiles of many heads are sooner done than parts are put together, and what is put together goes by the query heads.  More than 64 tiles
 // are the last to end.  (Whole / cut from 17 tiles on, us, sequences of 8 KV heads: 16 of 1000 10.6 / 12.5, 32 of 1800 15.3 / 18.8; 64 of 0 to 3632 of 4 KV heads 22.9 / 32.0.  64 of 0 to 1500, 2 KV heads of 128 of

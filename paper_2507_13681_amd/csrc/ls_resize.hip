@@ -3,11 +3,13 @@
 //
 // Everything follows from prefix sums over the sequences: of the rows that they add, of the pages that they need and of those that they give back.  A workgroup has 1024 sequences at a time, one a
 // thread, and every workgroup of a launch adds up all of them by itself (8 bytes a sequence, from the caches) rather than wait for another to do it; pages and rows are shared out among the
-// workgroups evenly, however unevenly the sequences have them, and which sequence one is of is found by bisecting the sums in LDS.
+// workgroups evenly, however unevenly the sequences have them, and which sequence one is of is found by bisecting the sums in LDS.  How many workgroups there are goes by the rows that a call has room
+// for, which is what the host knows: a step of up to 1024 rows has one (in place 8192), whatever comes back, and moves 1000 pages in a us.  (Contexts that end in a step of few rows, us: 24 of 512 pages 11.6, 64 of 512 27, 512 of
+// 2048 1032.)
 // Nobody waits for anybody: pages that are taken are read where those that are given back in the same call are not written, table entries that are read (of positions that were there) are none of those
 // that are written, and where lengths or the ring's state are updated in place by more than one workgroup, a launch of one more does that behind the others.
-// Bound by its launch and a chain of dependent loads (lengths, then pages, then rows), and of many sequences by the sums.  A decode step in place, us: 4 sequences 3.9, 256 4.6, 1024 5.6, 4096 17, 65535 292 (they
-// come 1024 at a time); sixteen sequences that grow by 23900 rows in all 4.7; 512 by 1.04 million rows 10.7 (13 MB: 2.5 of them).
+// Bound by its launch and a chain of dependent loads (lengths, then pages, then rows), and of many sequences by the sums.  A decode step in place, us: 4 sequences 3.9, 256 4.6, 1024 5.6, 4096 17, 65535 (of one KV head) 292 (they
+// come 1024 at a time); without starts, of 4 to 4096, 3.8, 3.8, 4.6, 13.4; sixteen sequences that grow by 23900 rows in all 4.7; 512 by 1.04 million rows 10.7 (13 MB: 2.5 of them).
 #include "ls_rows.h"
 
 namespace ls {

@@ -7,7 +7,7 @@
 // Angles.  A position times a frequency is formed in 64 bits and brought into a quarter turn there (t - k pi / 2 with pi / 2 in two parts): in 32 bits the angle of position 260000 would be off by up to
 // 2^-7.  Sine and cosine of what is left, at most pi / 4, are their series up to t^9 and t^10, whose next terms are below 2^-29.  The angles of a workgroup's rows are formed once, one or a few a
 // thread, and handed out through LDS: a workgroup has whole rows as far as it can (32 and 8 heads of 128: 4 rows of 40), since each row's 64 sines and cosines are as many instructions as the row itself.
-// 32 and 8 heads of 128, us: 32768 rows 128 (671 MB, 5.2 TB/s, a copy's rate; angles formed by each group of lanes for its heads of a row, 138), 23897 rows into rows and pages 122 (5.2 TB/s); a row of each of four sequences into
+// 32 and 8 heads of 128, us: 32768 rows 128 (671 MB, 5.2 TB/s, a copy's rate; angles formed by each group of lanes for its heads of a row, 138), 23897 rows into rows and pages 122 (5.2 TB/s), e4m3 129, e2m1 128 (4.5 and 4.4 TB/s, 114 and 110 at a copy's rate); a row of each of four sequences into
 // pages 4.2 (kernel 3.8; recorded into a graph 2.9), where an empty launch is 2.6.
 // Pages.  What a row becomes is rounded to the rows' type and then stored as ls_cache_write stores it, so that both ways give the same pages; 8 and 4 bits want
 // neighbouring values in a lane, which LDS brings together (a row's lanes are one wave's: no barrier).
